@@ -448,6 +448,120 @@ int snip_adamw_sensitivity(const float *m, const float *v, const void *g, int g_
                            float beta1, float beta2, float eps, double *sumsq, void *ws, size_t ws_bytes,
                            void *stream);
 
+/* ---- operators around the linears ---------------------------------------------------------- */
+
+/*
+ * RMS norm with the residual's addition, with the outputs that the linears behind it read.  (Fig. 5 starts
+ * from the X of a Llama-style block, Sec. 2.2; the paper does not define the norm, the rule below is the usual one.)
+ *   h = x + residual, rounded once to bf16 (h = x without a residual)
+ *   rstd = 1 / sqrt(mean_j h_j^2 + eps);   y_j = (h_j rstd) gain_j   in binary32
+ * Outputs, each produced where its pointer is given (at least one of them):
+ *   h       [rows][ld_h] bf16; required with a residual.  It may be x or residual themselves (same pointer and stride): the
+ *           stream is then updated in place.  Without a residual it must be NULL.
+ *   rstd    [rows]; what snip_rmsnorm_bwd reads.  Required with codes_t.
+ *   y       [rows][ld_y] bf16, rounded once.
+ *   codes, scales      : y quantized to fmt (FP8 or FP4) on 1x128 tiles: the layout of snip_quantize, SNIP_BLOCK_ROW_1x128, as stored
+ *   codes_t, scales_t  : y quantized to fmt_t on 128x1 tiles, stored transposed: SNIP_BLOCK_COL_128x1 with SNIP_Q_TRANSPOSED
+ * Scale and code rule are those of snip_quantize, applied to the binary32 y and not to its bf16 rounding (one rounding less than
+ * quantizing y; the codes of `codes` do not depend on which other outputs are asked for).
+ * rows: any number >= 0 (0: nothing is done); cols: a multiple of 8 up to 32768; a last tile is as long as what is left.
+ * With codes_t both must be multiples of 64, as the products behind it want them.  FP4 code buffers carry the slack of
+ * snip_quantize_sizes.  Strides: multiples of 8, >= cols.
+ * Inputs finite, with a mean of h^2 that binary32 holds; eps > 0.  Other outputs must overlap neither each other nor an input.
+ * No workspace.  Bytes per element: 2 (x) + 4 (residual, h) + 2 (y) + code and scale bytes of each copy; with
+ * codes_t h is read once more where it does not come out of the L2 cache.
+ */
+typedef struct {
+    const void *x;        /* bf16 [rows][ld_x] */
+    const void *residual; /* bf16 [rows][ld_residual] or NULL */
+    const void *gain;     /* [cols], gain_dtype */
+    void *h;
+    void *y;
+    float *rstd;
+    void *codes;
+    float *scales;
+    void *codes_t;
+    float *scales_t;
+    int64_t rows, cols, ld_x, ld_residual, ld_h, ld_y;
+    float eps;
+    int32_t gain_dtype;   /* SNIP_OUT_BF16 or SNIP_OUT_FP32 */
+    int32_t fmt, fmt_t;   /* snip_fmt_t; read where codes / codes_t are given */
+} snip_rmsnorm_t;
+int snip_rmsnorm_fwd(const snip_rmsnorm_t *args_host, void *stream);
+
+/*
+ * Its backward pass (quantization is passed straight through, as in the gradients of the linears):
+ *   g_j = dy_j gain_j;  c = mean_j g_j h_j rstd;  dx_j = rstd (g_j - h_j rstd c) + dresidual_j  (bf16, rounded once)
+ *   dgain_j = sum over rows of dy_j h_j rstd  (binary32; accumulate != 0 adds to what dgain holds)
+ * dx is the gradient of x and of residual alike (they enter as a sum); dresidual (may be NULL) is the gradient that reaches h by
+ * the residual stream.  dx may be dy or dresidual themselves (same pointer and stride); dgain may be NULL.  h, gain, rstd: as in the
+ * forward call (h = its x where it had no residual).  rows, cols, strides: as there; rows = 0 leaves dgain zero (or as it was, with
+ * accumulate).  Sums in binary32 in a fixed order that depends on the shape and the number of SMs only: reruns are bit-identical.
+ * ws: snip_rmsnorm_bwd_workspace bytes (0 and NULL without dgain); two calls that may run at the same time need one each.
+ * Bytes per element: 2 each for dy, h, dresidual and dx.
+ */
+typedef struct {
+    const void *dy;        /* bf16 [rows][ld_dy] */
+    const void *h;         /* bf16 [rows][ld_h] */
+    const void *gain;      /* [cols], gain_dtype */
+    const float *rstd;     /* [rows] */
+    const void *dresidual; /* bf16 [rows][ld_dresidual] or NULL */
+    void *dx;              /* bf16 [rows][ld_dx] */
+    float *dgain;          /* [cols] or NULL */
+    int64_t rows, cols, ld_dy, ld_h, ld_dresidual, ld_dx;
+    int32_t gain_dtype;
+    int32_t accumulate;
+} snip_rmsnorm_bwd_t;
+int snip_rmsnorm_bwd_workspace(int64_t rows, int64_t cols, size_t *ws_bytes_host);
+int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *args_host, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * One AdamW step (decoupled weight decay; the optimizer whose sensitivity snip_adamw_sensitivity measures, Sec. 4.3) over many
+ * tensors at once.  Per element, in binary32:
+ *   g' = grad * *grad_scale;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * The constants (1 - beta, bias corrections) are worked out in binary64.  All tensors of a call share param_dtype, grad_dtype and state_bits.
+ *   param        binary32 (master weights) or bf16, updated in place
+ *   param_bf16   optional: the new param rounded to nearest bf16 (what the quantizers read); binary32 params only
+ *   m, v         state_bits = 32: binary32.  state_bits = 8: one E4M3 code each, blocks of 128 consecutive elements (a tensor's last
+ *                may be shorter) with a binary32 scale by the rule of snip_quantize: m_scale / v_scale [ceil(n/128)];
+ *                m = value(code) / scale; v = (value(code) / scale)^2: what is coded is sqrt(v), which halves the span of magnitudes
+ *                that a block has to hold, and a positive v is never given code 0 (it would turn an update into m / eps).  A scale of
+ *                0 reads as a block of zeros, so that a state filled with zero bytes is a fresh one.
+ * rounding: of what is rounded to fewer than 32 bits and read back by the next step, i.e. 8-bit states and bf16 params.
+ * SNIP_ROUND_STOCHASTIC: the rule of snip_quantize_sr on the grid of the type concerned, with the generator's counter
+ * (q lo, q hi, t, 2 step + kind mod 2^32) for elements 4q..4q+3 of tensor t of the list, key = seed; kind 0: states, the
+ * 16-bit uniform of element i for m in bits [16 (i%2), +16) of output word i/2, for v in word 2 + i/2; kind 1: a bf16 param's, as for m.
+ * (Rounded to nearest, an 8-bit v stops moving once a step changes it by less than half a code; long runs want stochastic rounding.)
+ * step >= 1 counts this step.  step_device, lr_device (device, may be NULL) take the place of step and lr: a captured graph then reads
+ * the current values at each replay.  grad_scale (device, may be NULL = 1): inverse loss scale, clipping factor.
+ * Alignment: 16 bytes, scales 4.  n: any, 0 included.  Inputs finite.  The tensors must not overlap each other (what is written is
+ * written once).  No workspace; one launch per 448 tensors, read and written once per element.
+ */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale; /* state_bits = 8, else NULL */
+    void *param_bf16;         /* or NULL */
+    int64_t n;
+    float weight_decay;
+    int32_t reserved;
+} snip_adamw_tensor_t;
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;
+    const int64_t *step_device;
+    const float *lr_device;
+    const float *grad_scale;
+    uint64_t seed;
+    int32_t param_dtype, grad_dtype; /* SNIP_OUT_BF16 or SNIP_OUT_FP32 */
+    int32_t state_bits;              /* 32 or 8 */
+    int32_t rounding;                /* snip_rounding_t */
+} snip_adamw_t;
+int snip_adamw_state_sizes(int64_t n, int state_bits, size_t *state_bytes_host, size_t *scale_bytes_host);
+int snip_adamw_step(const snip_adamw_tensor_t *tensors_host, int64_t count, const snip_adamw_t *args_host, void *stream);
+
 /* ---- scheme generation, host side (paper Sec. 4.2, 4.3, 5) --------------------------------- */
 
 /*

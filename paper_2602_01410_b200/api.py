@@ -7,6 +7,7 @@ library is missing or fails to load, importing this module raises.
 """
 from __future__ import annotations
 
+import bisect
 import ctypes
 import os
 
@@ -27,7 +28,8 @@ LIB_PATH = os.environ.get("SNIP_B200_LIB") or os.path.join(os.path.dirname(os.pa
 EXPORTS = (
     "snip_version", "snip_status_string", "snip_last_cuda_error", "snip_quantize_sizes",
     "snip_quantize", "snip_quantize_noalloc", "snip_quantize_mx_sizes", "snip_quantize_mx", "snip_quantize_dual_workspace", "snip_quantize_dual", "snip_quantize_sr", "snip_workspace_size", "snip_gemm_quantized", "snip_gemm_mx", "snip_quantize_nvfp4_sizes", "snip_quantize_nvfp4_dual", "snip_gemm_nvfp4", "snip_linear_fwd_bwd_nvfp4_workspace", "snip_linear_fwd_bwd_nvfp4", "snip_linear_fwd",
-    "snip_linear_dgrad", "snip_linear_wgrad", "snip_linear_mx", "snip_linear_mx_workspace", "snip_linear_fwd_bwd_workspace", "snip_linear_fwd_bwd", "snip_layer_stats", "snip_layer_stats_workspace", "snip_adamw_sensitivity_workspace", "snip_adamw_sensitivity", "snip_loss_divergence", "snip_weight_divergence", "snip_select_scheme",
+    "snip_linear_dgrad", "snip_linear_wgrad", "snip_linear_mx", "snip_linear_mx_workspace", "snip_linear_fwd_bwd_workspace", "snip_linear_fwd_bwd", "snip_layer_stats", "snip_layer_stats_workspace", "snip_adamw_sensitivity_workspace", "snip_adamw_sensitivity",
+    "snip_rmsnorm_fwd", "snip_rmsnorm_bwd_workspace", "snip_rmsnorm_bwd", "snip_adamw_state_sizes", "snip_adamw_step", "snip_loss_divergence", "snip_weight_divergence", "snip_select_scheme",
     "snip_poll_status", "snip_debug_set", "snip_debug_last_gemm",
 )
 
@@ -60,6 +62,29 @@ GEMM_KERNEL_AUTO, GEMM_KERNEL_SINGLE, GEMM_KERNEL_PAIR, GEMM_KERNEL_NARROW = 0, 
 class LayerTensors(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("X", "W", "Y", "dY", "dX", "dW")] + \
                [(n, ctypes.c_int64) for n in ("M", "N", "K")]
+
+
+class RmsNorm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "gain", "h", "y", "rstd", "codes", "scales", "codes_t", "scales_t")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "ld_x", "ld_residual", "ld_h", "ld_y")] + \
+               [("eps", ctypes.c_float), ("gain_dtype", ctypes.c_int32), ("fmt", ctypes.c_int32), ("fmt_t", ctypes.c_int32)]
+
+
+class RmsNormBwd(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dy", "h", "gain", "rstd", "dresidual", "dx", "dgain")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "ld_dy", "ld_h", "ld_dresidual", "ld_dx")] + \
+               [("gain_dtype", ctypes.c_int32), ("accumulate", ctypes.c_int32)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "param_bf16")] + \
+               [("n", ctypes.c_int64), ("weight_decay", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class Adamw(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps")] + [("step", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("step_device", "lr_device", "grad_scale")] + [("seed", ctypes.c_uint64)] + \
+               [(n, ctypes.c_int32) for n in ("param_dtype", "grad_dtype", "state_bits", "rounding")]
 
 
 def _load():
@@ -100,6 +125,11 @@ def _load():
     lib.snip_layer_stats_workspace.argtypes = [i64, i64, i64, psz]
     lib.snip_adamw_sensitivity_workspace.argtypes = [i64, psz]
     lib.snip_adamw_sensitivity.argtypes = [vp, vp, vp, i32, i64, ctypes.c_float, ctypes.c_float, ctypes.c_float, vp, vp, sz, vp]
+    lib.snip_rmsnorm_fwd.argtypes = [ctypes.POINTER(RmsNorm), vp]
+    lib.snip_rmsnorm_bwd_workspace.argtypes = [i64, i64, psz]
+    lib.snip_rmsnorm_bwd.argtypes = [ctypes.POINTER(RmsNormBwd), vp, sz, vp]
+    lib.snip_adamw_state_sizes.argtypes = [i64, i32, psz, psz]
+    lib.snip_adamw_step.argtypes = [ctypes.POINTER(AdamwTensor), i64, ctypes.POINTER(Adamw), vp]
     dbl = ctypes.c_double
     lib.snip_loss_divergence.restype = dbl
     lib.snip_loss_divergence.argtypes = [dbl, dbl, i64, i64, dbl, dbl, i64, dbl]
@@ -494,6 +524,212 @@ def snip_adamw_sensitivity(m: torch.Tensor, v: torch.Tensor, g: torch.Tensor, be
     _check("snip_adamw_sensitivity", _lib.snip_adamw_sensitivity(_p(m), _p(v), _p(g), OUT_BF16 if g.dtype == torch.bfloat16 else OUT_FP32, n, beta1, beta2,
                                                                  eps, _p(out), _p(ws), ws.numel(), _stream()))
     return out
+
+
+def _require(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _same_device(tensors):
+    """Index of the one CUDA device that all of `tensors` (None: not given) are on."""
+    dev = None
+    for t in tensors:
+        if t is not None:
+            _require(t.is_cuda, "tensors have to be on a CUDA device")
+            d = t.get_device()
+            _require(dev is None or d == dev, "tensors have to be on one device")
+            dev = d
+    return dev
+
+
+def _call_on(dev, fn, call):
+    """call(stream) on device `dev`'s current stream, with `dev` current meanwhile."""
+    if dev is None or dev == torch.cuda.current_device():
+        _check(fn, call(_stream()))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn, call(_stream()))
+
+
+def _matrix(t, shape, name):
+    """Checks a bf16 matrix of `shape`; its row stride."""
+    _require(t.dtype == torch.bfloat16 and t.shape == shape, f"{name}: a bf16 tensor of shape {tuple(shape)} is wanted")
+    rows, cols = shape
+    _require(cols == 1 or t.stride(1) == 1, f"{name}: the elements of a row have to be adjacent")
+    return t.stride(0) if rows > 1 else cols   # a single row's stride says nothing
+
+
+def _vector(t, n, dtypes, name):
+    _require(t.dtype in dtypes and t.numel() == n and t.is_contiguous(), f"{name}: {n} contiguous elements of {' or '.join(map(str, dtypes))} are wanted")
+
+
+def _gain(t, cols):
+    _require(t.dim() == 1, "gain: a vector is wanted")
+    _vector(t, cols, (torch.bfloat16, torch.float32), "gain")
+    return OUT_BF16 if t.dtype == torch.bfloat16 else OUT_FP32
+
+
+_RMSNORM_OUTPUTS = frozenset(("h", "y", "rstd", "codes", "scales", "codes_t", "scales_t"))
+
+
+def _code_bytes(rows, cols, fmt):
+    """As snip_quantize_sizes, for any number of rows and a multiple of 8 columns."""
+    return rows * cols if fmt == FMT_FP8_E4M3 else rows * cols // 2 + (64 if rows % 128 or cols % 128 else 0)
+
+
+def snip_rmsnorm_fwd(x: torch.Tensor, gain: torch.Tensor, eps: float, *, residual=None, fmt=None, fmt_t=None, want_y=None, out=None):
+    """RMS norm of x + residual and its quantized copies.  Returns a dict: h (bf16, the sum; x itself without a residual), rstd (float32 [rows]),
+    y (bf16), codes / scales (row tiles, uint8 / float32), codes_t / scales_t (column tiles, stored transposed); None where not produced.
+    x, residual: bf16 [rows, cols], any row stride that is a multiple of 8.
+    Without `out`, buffers are allocated: codes if fmt is FMT_FP8_E4M3 or FMT_FP4_E2M1, codes_t if fmt_t is, y if want_y (default: no codes asked
+    for).  With `out`, a dict of such buffers, exactly those that it names are written (out["h"] may be residual or x: the sum in place)."""
+    _require(x.dim() == 2, "x: a matrix is wanted")
+    rows, cols = x.shape
+    if out is None:
+        def empty(n, dtype):
+            return torch.empty(n, dtype=dtype, device=x.device)
+
+        quant = (FMT_FP8_E4M3, FMT_FP4_E2M1)
+        _require(fmt in (None, FMT_BF16) + quant and fmt_t in (None, FMT_BF16) + quant, "fmt, fmt_t: FMT_FP8_E4M3, FMT_FP4_E2M1 or None")
+        out = {"h": None if residual is None else empty((rows, cols), torch.bfloat16), "rstd": empty(rows, torch.float32)}
+        if want_y or (want_y is None and fmt not in quant and fmt_t not in quant):
+            out["y"] = empty((rows, cols), torch.bfloat16)
+        if fmt in quant:
+            out["codes"], out["scales"] = empty(_code_bytes(rows, cols, fmt), torch.uint8), empty(-(-cols // 128) * rows, torch.float32)
+        if fmt_t in quant:
+            out["codes_t"], out["scales_t"] = empty(_code_bytes(rows, cols, fmt_t), torch.uint8), empty(-(-rows // 128) * cols, torch.float32)
+    else:
+        _require(want_y is None, "want_y: `out` says what is produced")
+        _require(_RMSNORM_OUTPUTS.issuperset(out), f"out: unknown outputs {sorted(set(out) - _RMSNORM_OUTPUTS)}")
+    get = out.get
+    h, y, rstd, codes, scales, codes_t, scales_t = get("h"), get("y"), get("rstd"), get("codes"), get("scales"), get("codes_t"), get("scales_t")
+    if residual is None and h is x:
+        h = None   # what an earlier call returned for h
+    _require((residual is None) == (h is None), "out: h goes with a residual")
+    a = RmsNorm(_p(x), _p(residual), _p(gain), _p(h), _p(y), _p(rstd), _p(codes), _p(scales), _p(codes_t), _p(scales_t), rows, cols, _matrix(x, x.shape, "x"),
+                0 if residual is None else _matrix(residual, x.shape, "residual"), 0 if h is None else _matrix(h, x.shape, "h"),
+                0 if y is None else _matrix(y, x.shape, "y"), eps, _gain(gain, cols), FMT_BF16 if fmt is None else fmt, FMT_BF16 if fmt_t is None else fmt_t)
+    if rstd is not None:
+        _vector(rstd, rows, (torch.float32,), "rstd")
+    for c, s, f, lines, along in ((codes, scales, fmt, rows, cols), (codes_t, scales_t, fmt_t, cols, rows)):
+        _require((c is None) == (s is None), "out: codes and scales go together")
+        if c is not None:
+            _require(f in (FMT_FP8_E4M3, FMT_FP4_E2M1), "codes are FMT_FP8_E4M3 or FMT_FP4_E2M1")
+            _require(c.dtype == torch.uint8 and c.is_contiguous() and c.numel() >= _code_bytes(rows, cols, f), "codes: too small, or not bytes")
+            _vector(s, -(-along // 128) * lines, (torch.float32,), "scales")
+    dev = _same_device((x, residual, gain, h, y, rstd, codes, scales, codes_t, scales_t))
+    _call_on(dev, "snip_rmsnorm_fwd", lambda st: _lib.snip_rmsnorm_fwd(ctypes.byref(a), st))
+    return {"h": x if h is None else h, "y": y, "rstd": rstd, "codes": codes, "scales": scales, "codes_t": codes_t, "scales_t": scales_t}
+
+
+def snip_rmsnorm_bwd_workspace(rows, cols):
+    n = ctypes.c_size_t()
+    _check("snip_rmsnorm_bwd_workspace", _lib.snip_rmsnorm_bwd_workspace(rows, cols, ctypes.byref(n)))
+    return n.value
+
+
+def snip_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd: torch.Tensor, *, dresidual=None, dx=None, dgain=None, want_dgain=True,
+                     accumulate=False, ws=None):
+    """Gradients of the norm: (dx, dgain).  dy, h, dresidual: bf16 [rows, cols]; h, rstd: of the forward call.  dx (bf16) may be dy or dresidual;
+    dgain: float32 [cols] (None with want_dgain=False), added to with accumulate."""
+    _require(dy.dim() == 2, "dy: a matrix is wanted")
+    rows, cols = dy.shape
+    if dx is None:
+        dx = torch.empty((rows, cols), dtype=torch.bfloat16, device=dy.device)
+    if dgain is None and want_dgain:
+        _require(not accumulate, "accumulate: needs the dgain to add to")
+        dgain = torch.empty(cols, dtype=torch.float32, device=dy.device)
+    a = RmsNormBwd(_p(dy), _p(h), _p(gain), _p(rstd), _p(dresidual), _p(dx), _p(dgain), rows, cols, _matrix(dy, dy.shape, "dy"), _matrix(h, dy.shape, "h"),
+                   0 if dresidual is None else _matrix(dresidual, dy.shape, "dresidual"), _matrix(dx, dy.shape, "dx"), _gain(gain, cols), int(accumulate))
+    _vector(rstd, rows, (torch.float32,), "rstd")
+    if dgain is not None:
+        _vector(dgain, cols, (torch.float32,), "dgain")
+        if ws is None:
+            ws = torch.empty(snip_rmsnorm_bwd_workspace(rows, cols), dtype=torch.uint8, device=dy.device)
+    if ws is not None:
+        _require(ws.is_contiguous(), "ws: contiguous memory is wanted")
+    dev = _same_device((dy, h, gain, rstd, dresidual, dx, dgain, ws))
+    size = 0 if ws is None else ws.numel() * ws.element_size()
+    _call_on(dev, "snip_rmsnorm_bwd", lambda st: _lib.snip_rmsnorm_bwd(ctypes.byref(a), _p(ws), size, st))
+    return dx, dgain
+
+
+def snip_adamw_state_sizes(n, state_bits):
+    """Bytes of one state tensor (m or v) of n elements, and of its scales."""
+    a, b = ctypes.c_size_t(), ctypes.c_size_t()
+    _check("snip_adamw_state_sizes", _lib.snip_adamw_state_sizes(n, state_bits, ctypes.byref(a), ctypes.byref(b)))
+    return a.value, b.value
+
+
+class AdamwTensors:
+    """The tensors of one AdamW step, checked and laid out for the library (make_adamw_tensors).  Holds the tensors."""
+
+    def __init__(self, table, count, device, param_dtype, grad_dtype, state_bits, keep):
+        self.table, self.count, self.device, self.param_dtype, self.grad_dtype, self.state_bits, self._keep = table, count, device, param_dtype, grad_dtype, state_bits, keep
+
+
+def make_adamw_tensors(params, grads, m, v, *, m_scales=None, v_scales=None, copies=None, weight_decay=0.0) -> AdamwTensors:
+    """Lists of contiguous CUDA tensors of one device, one entry per parameter.  params: float32 or bf16; grads: float32 or bf16; m, v: float32, or
+    uint8 (8-bit states) with m_scales, v_scales: float32, one value per 128 elements; copies: None, or a list of bf16 tensors (or None) that receive
+    the new float32 params; weight_decay: one number, or one per tensor.  Made once, used for as long as the tensors stay where they are (it holds them)."""
+    count = len(params)
+    lists = {"params": params, "grads": grads, "m": m, "v": v, "m_scales": m_scales, "v_scales": v_scales, "copies": copies}
+    decay = [weight_decay] * count if isinstance(weight_decay, (int, float)) else list(weight_decay)
+    for name, ts in lists.items():
+        _require(ts is None or len(ts) == count, f"{name}: one entry per parameter is wanted")
+    _require(len(decay) == count, "weight_decay: a number, or one per parameter")
+    lists = {name: [None] * count if ts is None else list(ts) for name, ts in lists.items()}
+    device = _same_device([t for ts in lists.values() for t in ts])
+    first = {name: next((t.dtype for t in ts if t is not None), None) for name, ts in lists.items()}
+    _require(first["params"] in (None, torch.float32, torch.bfloat16) and first["grads"] in (None, torch.float32, torch.bfloat16), "params, grads: float32 or bf16")
+    bits = 8 if first["m"] == torch.uint8 else 32
+    state = torch.uint8 if bits == 8 else torch.float32
+    written = []
+    table = (AdamwTensor * max(count, 1))()
+    for i in range(count):
+        n = lists["params"][i].numel()
+        wanted = {"params": (n, first["params"]), "grads": (n, first["grads"]), "m": (n, state), "v": (n, state)}
+        if bits == 8:
+            wanted |= {"m_scales": (-(-n // 128), torch.float32), "v_scales": (-(-n // 128), torch.float32)}
+        if lists["copies"][i] is not None:
+            _require(first["params"] == torch.float32, "copies: of float32 params")
+            wanted["copies"] = (n, torch.bfloat16)
+        row = {}
+        for name, ts in lists.items():
+            t = ts[i]
+            _require((t is not None) == (name in wanted), f"{name}[{i}]: {'missing' if t is None else 'not wanted'}")
+            if t is not None:
+                _vector(t, *wanted[name][:1], (wanted[name][1],), f"{name}[{i}]")
+                row[name] = t.data_ptr()
+                if t.numel() and name != "grads":
+                    written.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()))
+        table[i] = AdamwTensor(row["params"], row["grads"], row["m"], row["v"], row.get("m_scales"), row.get("v_scales"), row.get("copies"), n, decay[i], 0)
+    read = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in lists["grads"] if t.numel()]
+    written.sort()
+    _require(all(a[1] <= b[0] for a, b in zip(written, written[1:])), "tensors overlap: each may be given once")
+    starts = [w[0] for w in written]
+    for lo, hi in read:
+        k = bisect.bisect_left(starts, hi)
+        _require(k == 0 or written[k - 1][1] <= lo, "a gradient overlaps what the step writes")
+    return AdamwTensors(table, count, device, OUT_BF16 if first["params"] == torch.bfloat16 else OUT_FP32,
+                        OUT_BF16 if first["grads"] == torch.bfloat16 else OUT_FP32, bits, lists)
+
+
+def snip_adamw_step(tensors: AdamwTensors, lr, beta1: float, beta2: float, eps: float, step, *, rounding=ROUND_NEAREST_EVEN, seed=0, grad_scale=None):
+    """One AdamW step over `tensors` in place.  lr: a number, or a float32 CUDA tensor with one element; step: a whole number from 1, or an int64 CUDA
+    tensor with one element (both are then read when the step runs, also by each replay of a captured graph).  grad_scale: None, or a float32 CUDA tensor with one
+    element by which every gradient is multiplied."""
+    lr_dev, step_dev = lr if isinstance(lr, torch.Tensor) else None, step if isinstance(step, torch.Tensor) else None
+    for t, dtype, name in ((lr_dev, torch.float32, "lr"), (step_dev, torch.int64, "step"), (grad_scale, torch.float32, "grad_scale")):
+        if t is not None:
+            _vector(t, 1, (dtype,), name)
+            _require(t.is_cuda and (tensors.device is None or t.get_device() == tensors.device), f"{name}: not on the tensors' device")
+    _require(0 <= seed < 1 << 64, "seed: 64 bits")
+    a = Adamw(0.0 if lr_dev is not None else lr, beta1, beta2, eps, 0 if step_dev is not None else step, _p(step_dev), _p(lr_dev), _p(grad_scale), seed,
+              tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, rounding)
+    if tensors.count:
+        _call_on(tensors.device, "snip_adamw_step", lambda st: _lib.snip_adamw_step(tensors.table, tensors.count, ctypes.byref(a), st))
 
 
 def snip_loss_divergence(grad_x_norm, err_x_norm, M, K, grad_w_norm, err_w_norm, N, loss) -> float:

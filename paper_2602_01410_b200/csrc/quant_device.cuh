@@ -142,10 +142,9 @@ __device__ __forceinline__ float2 fp4_scaled_rounding_err(const float2 t)
 
 // ---- stochastic rounding (paper Sec. 6.1: FP4 output gradients) ------------------------------------
 
-// Philox4x32 with 10 rounds (Salmon et al., SC'11): counter (c0, c1, 0, 0), key (k0, k1).
-__device__ __forceinline__ void philox4x32_10(uint32_t c0, uint32_t c1, uint32_t k0, uint32_t k1, uint32_t (&out)[4])
+// Philox4x32 with 10 rounds (Salmon et al., SC'11): counter c, key (k0, k1).
+__device__ __forceinline__ void philox4x32_10(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1, uint32_t (&out)[4])
 {
-    uint32_t c2 = 0, c3 = 0;
 #pragma unroll
     for (int round = 0; round < 10; ++round) {
         const uint32_t hi0 = __umulhi(0xD2511F53u, c0), lo0 = 0xD2511F53u * c0;
@@ -154,6 +153,11 @@ __device__ __forceinline__ void philox4x32_10(uint32_t c0, uint32_t c1, uint32_t
         k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
     }
     out[0] = c0; out[1] = c1; out[2] = c2; out[3] = c3;
+}
+// ... counter (c0, c1, 0, 0)
+__device__ __forceinline__ void philox4x32_10(uint32_t c0, uint32_t c1, uint32_t k0, uint32_t k1, uint32_t (&out)[4])
+{
+    philox4x32_10(c0, c1, 0u, 0u, k0, k1, out);
 }
 
 // The 16-bit uniforms of an element pair (first element low) in the form sr_e2m1_value takes: 64 (65535 - u) + 31.
