@@ -535,6 +535,7 @@ int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *args_host, void *ws, size_t ws_by
  * (Rounded to nearest, an 8-bit v stops moving once a step changes it by less than half a code; long runs want stochastic rounding.)
  * step >= 1 counts this step.  step_device, lr_device (device, may be NULL) take the place of step and lr: a captured graph then reads
  * the current values at each replay.  grad_scale (device, may be NULL = 1): inverse loss scale, clipping factor.
+ * eps: a normal binary32 number.  The root of a v below 2^-126 comes out too small (0 stays 0).
  * Alignment: 16 bytes, scales 4.  n: any, 0 included.  Inputs finite.  The tensors must not overlap each other (what is written is
  * written once).  No workspace; one launch per 448 tensors, read and written once per element.
  */

@@ -1,14 +1,19 @@
 // One AdamW step over many tensors at once, states in 32 or 8 bits.
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
-// Bound by HBM: 28 bytes per element with binary32 states (p, g, m, v, bf16 copy; read and written once), 16 with 8-bit ones.
+// Bound by HBM: 28 bytes per element with binary32 states (p, bf16 g, m, v, bf16 copy; read and written once), 16 with 8-bit ones, which also need
+// 50 (nearest) to 70 (stochastic) instructions per element: arithmetic on pairs, a warp's loads all ahead of its arithmetic.  Fetching the next
+// chunk into shared memory meanwhile (cp.async) costs more instructions and registers than it hides (SR: 703 us in the place of 605).  Loads and
+// stores without cache hints: streaming stores cost 4 % (846 / 809 us on four 1B blocks).
 // The tensors' table travels in the kernel's parameters, so that a call needs no device memory of its own and a captured graph holds it;
-// a chunk of 4096 elements is the unit of work, the resident grid walks over the chunks of all tensors, and a chunk's tensor is found by
+// a chunk of 2048 elements is the unit of work, the resident grid walks over the chunks of all tensors, and a chunk's tensor is found by
 // bisection in the table.  A warp holds 128 consecutive elements at a time, four per lane: that is a block of the 8-bit states, whose
 // maximum is then one warp-wide integer reduction (magnitudes order like their bits).
 #include <cuda_bf16.h>
 #include <float.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "common.cuh"
 #include "quant_device.cuh"
@@ -19,9 +24,9 @@ int gemm_sm_count();
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kBlock = 128;      // elements that share a scale
-constexpr int kChunk = 4096;     // elements a CTA takes at a time
+constexpr int kChunk = 2048;     // elements a CTA takes at a time
 constexpr int kMostTensors = 448;
 constexpr int kFewTensors = 16;
 
@@ -43,7 +48,7 @@ struct Common {
     Hyper h;                             // without device values
     const int64_t *step_device;
     const float *lr_device, *grad_scale;
-    uint64_t seed;
+    uint32_t k0, k1;                     // the generator's key
     uint32_t step;
     uint32_t chunks;
     int32_t count, first_tensor;
@@ -62,232 +67,377 @@ __host__ __device__ inline Hyper hyper(double lr, double beta1, double beta2, in
     return {(float)(lr / bc1), (float)(1.0 / sqrt(bc2)), (float)lr};
 }
 
-// Stochastically rounded E4M3 value of t for the 16-bit uniform u: with a = min(|t|, 448), lo <= a < hi the neighbouring grid points, hi iff
-// (a - lo)/(hi - lo) > (u + 1/2)/2^16.  On the bits, as for E2M1: from 2^-6 up a grid point has 20 zero bits at its end, and their
-// value f exceeds 16 u + 8 iff f + 16 (65535 - u) + 7 carries out of them; below, the same holds for a + 2^-6, rounded upwards.
-__device__ __forceinline__ float sr_e4m3_value(float t, uint32_t u)
+// Stochastic rounding of a pair of values to E4M3, by one 32-bit word of the generator (its low half for the first): with a = |t|, lo <= a < hi
+// the neighbouring grid points and u the 16-bit uniform, hi iff (a - lo)/(hi - lo) > (u + 1/2)/2^16.  On the bits of 64 a, as for E2M1: from
+// 1 up a grid point has 20 zero bits at its end, and their value f exceeds 16 u + 8 iff f + 16 (65535 - u) + 7 carries out of them; below,
+// the same holds for 64 a + 1, rounded upwards.  t comes from a block scaled by its own maximum: it passes 448 by a few last places at
+// most, which leave the largest addend 9 units short of a carry.  SIGNED = false: t >= 0.
+template <bool SIGNED>
+__device__ __forceinline__ float2 sr_e4m3x2(const float2 t, uint32_t w)
 {
-    const float a = fminf(fabsf(t), 448.0f);
-    const float off = a < 0.015625f ? 0.015625f : 0.0f;
-    const uint32_t q = (__float_as_uint(__fadd_ru(a, off)) + ((65535u - u) * 16u + 7u)) & 0xFFF00000u;
-    return copysignf(__uint_as_float(q) - off, t);
+    const float2 b = __fmul2_rn(t, make_float2(64.0f, 64.0f)), a = SIGNED ? make_float2(fabsf(b.x), fabsf(b.y)) : b;
+    float2 off;   // 1 below 1, else 0, on the FMA pipe (a comparison and a selection per value on the integer pipe: 602 against 598 us)
+    asm("fma.rn.sat.f32 %0, %1, 0fFB800000, 0f7B800000;" : "=f"(off.x) : "f"(a.x));
+    asm("fma.rn.sat.f32 %0, %1, 0fFB800000, 0f7B800000;" : "=f"(off.y) : "f"(a.y));
+    const float2 s = __fadd2_ru(a, off);
+    const uint32_t r0 = ((~w << 4) & 0xFFFF0u) | 7u, r1 = ((~w >> 12) & 0xFFFF0u) | 7u;
+    const float2 q = make_float2(__uint_as_float((__float_as_uint(s.x) + r0) & 0xFFF00000u), __uint_as_float((__float_as_uint(s.y) + r1) & 0xFFF00000u));
+    const float2 v = __ffma2_rn(q, make_float2(0.015625f, 0.015625f), __fmul2_rn(off, make_float2(-0.015625f, -0.015625f)));
+    return SIGNED ? make_float2(copysignf(v.x, t.x), copysignf(v.y, t.y)) : v;
 }
-// ... and of a bf16 value, as binary32: the low 16 bits f exceed u + 1/2 iff f + 65535 - u carries.
-__device__ __forceinline__ uint32_t sr_bf16_bits(float t, uint32_t u) { return (__float_as_uint(t) + (65535u - u)) >> 16; }
-
-__device__ __forceinline__ uint32_t warp_max(float a0, float a1, float a2, float a3)
+// ... to bf16 bits, packed: the low 16 bits f exceed u + 1/2 iff f + 65535 - u carries.
+__device__ __forceinline__ uint32_t sr_bf16x2(const float2 t, uint32_t w)
 {
-    return __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(fmaxf(a0, a1), fmaxf(a2, a3))));
+    const uint32_t lo = __float_as_uint(t.x) + (~w & 0xFFFFu), hi = __float_as_uint(t.y) + (~w >> 16);
+    return __byte_perm(lo, hi, 0x7632);
 }
-
-__device__ __forceinline__ float sqrt_fast(float v)
+__device__ __forceinline__ uint32_t rn_bf16x2(const float2 t)
 {
-    float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(t.y), "f"(t.x));
     return r;
 }
 
-// Four consecutive elements of a lane; `left`: how many of them the tensor has.
-template <bool BF16>
-__device__ __forceinline__ void load4(const void *p, int64_t i, int left, float (&f)[4])
+__device__ __forceinline__ float rcp_fast(float x)
 {
-    if constexpr (BF16) {
-        const uint16_t *q = static_cast<const uint16_t *>(p) + i;
-        if (left >= 4) {
-            const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(q));
-            f[0] = bf16lo(v.x); f[1] = bf16hi(v.x); f[2] = bf16lo(v.y); f[3] = bf16hi(v.y);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = j < left ? __uint_as_float((uint32_t)q[j] << 16) : 0.0f;
-        }
-    } else {
-        const float *q = static_cast<const float *>(p) + i;
-        if (left >= 4) {
-            const float4 v = __ldcs(reinterpret_cast<const float4 *>(q));
-            f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = j < left ? q[j] : 0.0f;
-        }
-    }
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
-__device__ __forceinline__ void store4(float *p, int64_t i, int left, const float (&f)[4])
+// Square roots to half a last place: v times its approximate reciprocal root, and a Newton step.  (Below 2^-126, where the reciprocal root is
+// held at 2^63, too small; 0 for 0.)
+__device__ __forceinline__ float2 sqrt2(const float2 v)
 {
+    float2 y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, FLT_MIN)));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(v.y, FLT_MIN)));
+    const float2 s = __fmul2_rn(v, y), h = __fmul2_rn(y, make_float2(-0.5f, -0.5f));
+    const float2 d = __ffma2_rn(s, s, make_float2(-v.x, -v.y));
+    return __ffma2_rn(d, h, s);
+}
+
+__device__ __forceinline__ float2 unpack2(uint32_t b) { return make_float2(bf16lo(b), bf16hi(b)); }
+
+// Four consecutive elements of a lane, of which the tensor has `left` (the others read as zeros).
+__device__ __forceinline__ void load4(const void *p, uint32_t i, int left, uint2 &v)
+{
+    const uint16_t *q = static_cast<const uint16_t *>(p) + i;
     if (left >= 4) {
-        __stcs(reinterpret_cast<float4 *>(p + i), make_float4(f[0], f[1], f[2], f[3]));
+        v = *reinterpret_cast<const uint2 *>(q);
     } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < left) p[i + j] = f[j];
+        v = make_uint2(0u, 0u);
+        if (left > 0) v.x = q[0];
+        if (left > 1) v.x |= (uint32_t)q[1] << 16;
+        if (left > 2) v.y = q[2];
     }
 }
-__device__ __forceinline__ void store4(uint16_t *p, int64_t i, int left, const uint32_t (&b)[4])
+__device__ __forceinline__ void load4(const void *p, uint32_t i, int left, float4 &v)
 {
+    const float *q = static_cast<const float *>(p) + i;
     if (left >= 4) {
-        *reinterpret_cast<uint2 *>(p + i) = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
+        v = *reinterpret_cast<const float4 *>(q);
     } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < left) p[i + j] = (uint16_t)b[j];
+        v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (left > 0) v.x = q[0];
+        if (left > 1) v.y = q[1];
+        if (left > 2) v.z = q[2];
     }
 }
-__device__ __forceinline__ uint32_t load_codes(const void *p, int64_t i, int left)
+__device__ __forceinline__ uint32_t load_codes(const uint8_t *p, uint32_t i, int left)
 {
-    const uint8_t *q = static_cast<const uint8_t *>(p) + i;
-    if (left >= 4) return __ldcs(reinterpret_cast<const uint32_t *>(q));
+    if (left >= 4) return *reinterpret_cast<const uint32_t *>(p + i);
     uint32_t v = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (j < left) v |= (uint32_t)q[j] << (8 * j);
+    for (int j = 0; j < 3; ++j)
+        if (j < left) v |= (uint32_t)p[i + j] << (8 * j);
     return v;
 }
-__device__ __forceinline__ void store_codes(void *p, int64_t i, int left, uint32_t v)
+__device__ __forceinline__ void to_floats(const uint2 &v, float2 (&f)[2]) { f[0] = unpack2(v.x); f[1] = unpack2(v.y); }
+__device__ __forceinline__ void to_floats(const float4 &v, float2 (&f)[2]) { f[0] = make_float2(v.x, v.y); f[1] = make_float2(v.z, v.w); }
+template <bool BF16>
+using Vec = std::conditional_t<BF16, uint2, float4>;
+template <bool FULL>
+__device__ __forceinline__ void store4(float *p, uint32_t i, int left, const float2 (&f)[2])
 {
-    uint8_t *q = static_cast<uint8_t *>(p) + i;
-    if (left >= 4) {
-        __stcs(reinterpret_cast<uint32_t *>(q), v);
+    if (FULL) {
+        *reinterpret_cast<float4 *>(p + i) = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+    } else {
+        if (left > 0) p[i] = f[0].x;
+        if (left > 1) p[i + 1] = f[0].y;
+        if (left > 2) p[i + 2] = f[1].x;
+        if (left > 3) p[i + 3] = f[1].y;
+    }
+}
+template <bool FULL>
+__device__ __forceinline__ void store4(uint16_t *p, uint32_t i, int left, uint32_t b0, uint32_t b1)
+{
+    if (FULL) {
+        *reinterpret_cast<uint2 *>(p + i) = make_uint2(b0, b1);
+    } else {
+        if (left > 0) p[i] = (uint16_t)b0;
+        if (left > 1) p[i + 1] = (uint16_t)(b0 >> 16);
+        if (left > 2) p[i + 2] = (uint16_t)b1;
+        if (left > 3) p[i + 3] = (uint16_t)(b1 >> 16);
+    }
+}
+template <bool FULL>
+__device__ __forceinline__ void store_codes(uint8_t *p, uint32_t i, int left, uint32_t v)
+{
+    if (FULL) {
+        *reinterpret_cast<uint32_t *>(p + i) = v;
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (j < left) q[j] = (uint8_t)(v >> (8 * j));
+            if (j < left) p[i + j] = (uint8_t)(v >> (8 * j));
     }
 }
-__device__ __forceinline__ uint32_t bf16_bits(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
 
-// What a lane holds of one block.
-template <bool BITS8>
-struct Four {
-    float p[4], g[4];
-    float m[BITS8 ? 1 : 4], v[BITS8 ? 1 : 4];
-    uint32_t mc, vc;
-    float ms, vs;
-    int left;
+// The numbers of a step, the same for every element of a tensor.
+struct Step {
+    Hyper h;
+    float b1, omb1, b2, omb2, eps, gs, keep;
+    uint32_t k0, k1, tensor, count;   // of the generator: key, counter words 2 and 3 (without the kind)
 };
 
+// A chunk of a tensor: pointers to its first element.
+struct Chunk {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    uint16_t *param_bf16;
+    uint64_t quad;    // number of its first four elements in the tensor
+    int32_t left;     // elements of the tensor from here on, if fewer than a chunk
+};
+
+__device__ __forceinline__ float2 splat(float x) { return make_float2(x, x); }
+
+// The generator's words for the four elements at i.  A chunk's groups of four share the upper word of their number.
+__device__ __forceinline__ void generator(const Step &s, const Chunk &c, uint32_t i, uint32_t kind, uint32_t (&w)[4])
+{
+    philox4x32_10((uint32_t)c.quad + (i >> 2), (uint32_t)(c.quad >> 32), s.tensor, s.count + kind, s.k0, s.k1, w);
+}
+
+// m and r = sqrt(v) (v itself in `v`), and the new weights, of four elements.
+__device__ __forceinline__ void update4(const Step &s, float2 (&p)[2], const float2 (&g)[2], float2 (&m)[2], float2 (&v)[2], float2 (&r)[2])
+{
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        // m, v hold b1 m and b2 v on entry
+        const float2 gg = __fmul2_rn(g[j], splat(s.gs));
+        m[j] = __ffma2_rn(gg, splat(s.omb1), m[j]);
+        v[j] = __ffma2_rn(__fmul2_rn(gg, splat(s.omb2)), gg, v[j]);
+        r[j] = sqrt2(v[j]);
+        const float2 d = __ffma2_rn(r[j], splat(s.h.inv_sqrt_bc2), splat(s.eps));
+        const float2 u = __fmul2_rn(__fmul2_rn(m[j], splat(-s.h.step_size)), make_float2(rcp_fast(d.x), rcp_fast(d.y)));
+        p[j] = __ffma2_rn(p[j], splat(s.keep), u);
+    }
+}
+
+template <bool FULL, bool P_BF16, bool SR>
+__device__ __forceinline__ void store_param(const Step &s, const Chunk &c, uint32_t i, int left, const float2 (&p)[2])
+{
+    if constexpr (P_BF16) {
+        uint32_t b0, b1;
+        if constexpr (SR) {
+            uint32_t w[4];
+            generator(s, c, i, 1, w);
+            b0 = sr_bf16x2(p[0], w[0]);
+            b1 = sr_bf16x2(p[1], w[1]);
+        } else {
+            b0 = rn_bf16x2(p[0]);
+            b1 = rn_bf16x2(p[1]);
+        }
+        store4<FULL>(static_cast<uint16_t *>(c.param), i, left, b0, b1);
+    } else {
+        store4<FULL>(static_cast<float *>(c.param), i, left, p);
+        if (c.param_bf16) store4<FULL>(c.param_bf16, i, left, rn_bf16x2(p[0]), rn_bf16x2(p[1]));
+    }
+}
+
+constexpr int kWarps = kThreads / 32;
+
+// A warp's share of a chunk, binary32 states.
+template <bool FULL, bool P_BF16, bool G_BF16, bool SR>
+__device__ __forceinline__ void run_chunk32(const Step &s, const Chunk &c, int warp, int lane)
+{
+#pragma unroll 1
+    for (int part = 0; part < kChunk / (kBlock * kWarps); ++part) {
+        const uint32_t i = (uint32_t)((part * kWarps + warp) * kBlock + 4 * lane);
+        const int left = FULL ? 4 : c.left - (int)i;
+        Vec<P_BF16> pv;
+        Vec<G_BF16> gv;
+        float4 mv, vv;
+        load4(c.param, i, left, pv);
+        load4(c.grad, i, left, gv);
+        load4(c.m, i, left, mv);
+        load4(c.v, i, left, vv);
+        float2 p[2], g[2], m[2], v[2], r[2];
+        to_floats(pv, p);
+        to_floats(gv, g);
+        to_floats(mv, m);
+        to_floats(vv, v);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            m[j] = __fmul2_rn(m[j], splat(s.b1));
+            v[j] = __fmul2_rn(v[j], splat(s.b2));
+        }
+        update4(s, p, g, m, v, r);
+        store4<FULL>(static_cast<float *>(c.m), i, left, m);
+        store4<FULL>(static_cast<float *>(c.v), i, left, v);
+        store_param<FULL, P_BF16, SR>(s, c, i, left, p);
+    }
+}
+
+// ... 8-bit states.  What is done once per block and state (reading a scale and dividing by it, making the new one) is done by one lane each:
+// lanes 0 .. U-1 for the first moments of the warp's U blocks, lanes U .. 2 U - 1 for the second, and handed round by shuffles.
+template <bool FULL, bool P_BF16, bool G_BF16, bool SR>
+__device__ __forceinline__ void run_chunk8(const Step &s, const Chunk &c, int warp, int lane)
+{
+    constexpr int U = kChunk / (kBlock * kWarps);
+    constexpr uint32_t kAll = 0xFFFFFFFFu;
+    const uint32_t b0 = (uint32_t)(warp * U), i0 = b0 * kBlock + 4 * lane;
+    if (!FULL && (int)(b0 * kBlock) >= c.left) return;     // the whole warp
+    Vec<P_BF16> pv[U];
+    Vec<G_BF16> gv[U];
+    uint32_t mc[U], vc[U];
+    const bool second = (lane & U) != 0;
+    float *scales = second ? c.v_scale : c.m_scale;
+    const uint32_t block = b0 + (lane & (U - 1));
+    const bool owner = lane < 2 * U && (FULL || (int)(block * kBlock) < c.left);
+    const float scale = owner ? scales[block] : 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t i = i0 + u * kBlock;
+        const int left = FULL ? 4 : c.left - (int)i;
+        load4(c.param, i, left, pv[u]);
+        load4(c.grad, i, left, gv[u]);
+        mc[u] = load_codes(static_cast<const uint8_t *>(c.m), i, left);
+        vc[u] = load_codes(static_cast<const uint8_t *>(c.v), i, left);
+    }
+    // b1 m = code (b1 / S);  b2 v = (code / S) (code b2 / S)
+    const float inv = scale == 0.0f ? 0.0f : __frcp_rn(scale), d1 = second ? inv : s.b1 * inv, d2 = s.b2 * inv;
+    float2 m[U][2], r[U][2];
+    float most = 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t i = i0 + u * kBlock;
+        const float b1s = __shfl_sync(kAll, d1, u), vs = __shfl_sync(kAll, d1, U + u), b2s = __shfl_sync(kAll, d2, U + u);
+        float2 p[2], g[2], v[2];
+        to_floats(pv[u], p);
+        to_floats(gv[u], g);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            m[u][j] = __fmul2_rn(dec_e4m3x2(mc[u] >> (16 * j)), splat(b1s));
+            const float2 code = dec_e4m3x2(vc[u] >> (16 * j));
+            v[j] = __fmul2_rn(__fmul2_rn(code, splat(vs)), __fmul2_rn(code, splat(b2s)));
+        }
+        update4(s, p, g, m[u], v, r[u]);
+        store_param<FULL, P_BF16, SR>(s, c, i, FULL ? 4 : c.left - (int)i, p);
+        // magnitudes order like their bits
+        const uint32_t am = __reduce_max_sync(kAll, __float_as_uint(fmaxf(fmaxf(fabsf(m[u][0].x), fabsf(m[u][0].y)), fmaxf(fabsf(m[u][1].x), fabsf(m[u][1].y)))));
+        const uint32_t ar = __reduce_max_sync(kAll, __float_as_uint(fmaxf(fmaxf(r[u][0].x, r[u][0].y), fmaxf(r[u][1].x, r[u][1].y))));
+        if ((lane & (U - 1)) == u) most = __uint_as_float(second ? ar : am);
+    }
+    const float fresh = tile_scale<SNIP_FMT_FP8_E4M3>(most, 0);
+    if (owner) scales[block] = fresh;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t i = i0 + u * kBlock;
+        const int left = FULL ? 4 : c.left - (int)i;
+        const float sm = __shfl_sync(kAll, fresh, u), sv = __shfl_sync(kAll, fresh, U + u);
+        float2 tm[2], tv[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            tm[j] = __fmul2_rn(m[u][j], splat(sm));
+            tv[j] = __fmul2_rn(r[u][j], splat(sv));
+        }
+        if constexpr (SR) {
+            uint32_t w[4];
+            generator(s, c, i, 0, w);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                tm[j] = sr_e4m3x2<true>(tm[j], w[j]);
+                tv[j] = sr_e4m3x2<false>(tv[j], w[2 + j]);
+            }
+        }
+        uint32_t codes = cvt_e4m3x2(tv[0].x, tv[0].y) | cvt_e4m3x2(tv[1].x, tv[1].y) << 16;
+        if ((codes - 0x01010101u) & 0x80808080u) {   // perhaps a code 0 (a code has 7 bits): what is positive gets the smallest one instead
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float rj = j & 1 ? r[u][j >> 1].y : r[u][j >> 1].x;
+                if (((codes >> (8 * j)) & 0xFFu) == 0u && rj > 0.0f) codes |= 1u << (8 * j);
+            }
+        }
+        store_codes<FULL>(static_cast<uint8_t *>(c.m), i, left, cvt_e4m3x2(tm[0].x, tm[0].y) | cvt_e4m3x2(tm[1].x, tm[1].y) << 16);
+        store_codes<FULL>(static_cast<uint8_t *>(c.v), i, left, codes);
+    }
+}
+
+// The tensor that a chunk belongs to, and the chunk in it.
+template <int CAP, bool P_BF16, bool G_BF16, bool BITS8>
+__device__ __forceinline__ int locate(const Table<CAP> &a, uint32_t chunk, Chunk &k)
+{
+    int lo = 0, hi = a.c.count;       // last entry whose first chunk is not behind this one
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.e[mid].first_chunk <= chunk) lo = mid;
+        else hi = mid;
+    }
+    const Entry &e = a.e[lo];
+    const int64_t base = (int64_t)(chunk - e.first_chunk) * kChunk, left = e.n - base;
+    k.param = static_cast<uint8_t *>(e.param) + base * (P_BF16 ? 2 : 4);
+    k.grad = static_cast<const uint8_t *>(e.grad) + base * (G_BF16 ? 2 : 4);
+    k.m = static_cast<uint8_t *>(e.m) + base * (BITS8 ? 1 : 4);
+    k.v = static_cast<uint8_t *>(e.v) + base * (BITS8 ? 1 : 4);
+    k.m_scale = e.m_scale + base / kBlock;
+    k.v_scale = e.v_scale + base / kBlock;
+    k.param_bf16 = e.param_bf16 ? e.param_bf16 + base : nullptr;
+    k.quad = (uint64_t)base >> 2;
+    k.left = left < kChunk ? (int32_t)left : kChunk;
+    return lo;
+}
+
+// CTAs per SM that the registers are cut for.  A 7B block (202 M elements) in us, at five / six / seven: 8-bit states to nearest 544 / 569 / 567
+// with binary32 weights, 377 / 354 / 340 with bf16 ones; stochastic 609 / 598 / 580 and 695 / 722 / 739 (two generator calls per four elements:
+// fewer registers spill).  Binary32 states: six keep 24 warps of one block each in flight; two blocks per warp or more warps are no faster.
+constexpr int resident_ctas(bool p16, bool bits8, bool sr)
+{
+    return !bits8 ? 6 : p16 == sr ? 5 : 7;
+}
+
 template <int CAP, bool P_BF16, bool G_BF16, bool BITS8, bool SR>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Table<CAP> a)
+__global__ void __launch_bounds__(kThreads, resident_ctas(P_BF16, BITS8, SR)) adamw_kernel(const __grid_constant__ Table<CAP> a)
 {
     __shared__ Hyper shared_hyper;
     const Common &c = a.c;
-    Hyper h = c.h;
+    Step s;
+    s.h = c.h;
     uint32_t step = c.step;
     if (c.step_device || c.lr_device) {
         const int64_t t = c.step_device ? *c.step_device : (int64_t)c.step;
         if (threadIdx.x == 0) shared_hyper = hyper(c.lr_device ? (double)*c.lr_device : c.lr, c.beta1, c.beta2, t);
         __syncthreads();
-        h = shared_hyper;
+        s.h = shared_hyper;
         step = (uint32_t)t;
     }
-    const float gs = c.grad_scale ? *c.grad_scale : 1.0f;
+    s.b1 = c.b1; s.omb1 = c.omb1; s.b2 = c.b2; s.omb2 = c.omb2; s.eps = c.eps;
+    s.gs = c.grad_scale ? *c.grad_scale : 1.0f;
+    s.k0 = c.k0; s.k1 = c.k1;
+    s.count = 2u * step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int U = BITS8 ? 4 : 2;    // blocks in flight per warp
-    constexpr int kWarps = kThreads / 32;
     for (uint32_t chunk = blockIdx.x; chunk < c.chunks; chunk += gridDim.x) {
-        int lo = 0, hi = c.count;       // last entry whose first chunk is not behind this one
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (a.e[mid].first_chunk <= chunk) lo = mid;
-            else hi = mid;
-        }
-        const Entry &e = a.e[lo];
-        const int64_t base = (int64_t)(chunk - e.first_chunk) * kChunk;
-        const float keep = (float)(1.0 - (double)h.lr * (double)e.weight_decay);
-#pragma unroll 1
-        for (int part = 0; part < kChunk / (kBlock * kWarps * U); ++part) {
-            Four<BITS8> x[U];
-            const int64_t b0 = base + (int64_t)(part * U * kWarps + warp) * kBlock;   // U blocks, kWarps apart
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t b = b0 + u * kWarps * kBlock, i = b + 4 * lane;
-                const int64_t rest = e.n - i;
-                x[u].left = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
-                load4<P_BF16>(e.param, i, x[u].left, x[u].p);
-                load4<G_BF16>(e.grad, i, x[u].left, x[u].g);
-                if constexpr (BITS8) {
-                    x[u].mc = load_codes(e.m, i, x[u].left);
-                    x[u].vc = load_codes(e.v, i, x[u].left);
-                    x[u].ms = x[u].vs = 0.0f;
-                    if (b < e.n) { x[u].ms = e.m_scale[b / kBlock]; x[u].vs = e.v_scale[b / kBlock]; }
-                } else {
-                    load4<false>(e.m, i, x[u].left, x[u].m);
-                    load4<false>(e.v, i, x[u].left, x[u].v);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t b = b0 + u * kWarps * kBlock, i = b + 4 * lane;
-                if (b >= e.n) break;    // the whole warp
-                const int left = x[u].left;
-                float m[4], v[4], r[4], p[4];
-                if constexpr (BITS8) {
-                    const float im = x[u].ms == 0.0f ? 0.0f : __frcp_rn(x[u].ms), iv = x[u].vs == 0.0f ? 0.0f : __frcp_rn(x[u].vs);
-                    const float2 m0 = dec_e4m3x2(x[u].mc), m1 = dec_e4m3x2(x[u].mc >> 16), v0 = dec_e4m3x2(x[u].vc), v1 = dec_e4m3x2(x[u].vc >> 16);
-                    m[0] = m0.x * im; m[1] = m0.y * im; m[2] = m1.x * im; m[3] = m1.y * im;
-                    v[0] = v0.x * iv; v[1] = v0.y * iv; v[2] = v1.x * iv; v[3] = v1.y * iv;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] *= v[j];
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) { m[j] = x[u].m[j]; v[j] = x[u].v[j]; }
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float g = x[u].g[j] * gs;
-                    m[j] = fmaf(c.b1, m[j], c.omb1 * g);
-                    v[j] = fmaf(c.b2, v[j], c.omb2 * g * g);
-                    r[j] = sqrt_fast(v[j]);
-                    p[j] = fmaf(x[u].p[j], keep, -h.step_size * __fdividef(m[j], fmaf(r[j], h.inv_sqrt_bc2, c.eps)));
-                }
-                const uint64_t q = (uint64_t)i >> 2;
-                const uint32_t tensor = (uint32_t)(c.first_tensor + lo);
-                if constexpr (BITS8) {
-                    const float am = __uint_as_float(warp_max(fabsf(m[0]), fabsf(m[1]), fabsf(m[2]), fabsf(m[3])));
-                    const float ar = __uint_as_float(warp_max(r[0], r[1], r[2], r[3]));
-                    const float sm = tile_scale<SNIP_FMT_FP8_E4M3>(am, 0), sv = tile_scale<SNIP_FMT_FP8_E4M3>(ar, 0);
-                    float tm[4], tv[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) { tm[j] = m[j] * sm; tv[j] = r[j] * sv; }
-                    if constexpr (SR) {
-                        uint32_t w[4];
-                        philox4x32_10((uint32_t)q, (uint32_t)(q >> 32), tensor, 2u * step, (uint32_t)c.seed, (uint32_t)(c.seed >> 32), w);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            tm[j] = sr_e4m3_value(tm[j], (w[j >> 1] >> (16 * (j & 1))) & 0xFFFFu);
-                            tv[j] = sr_e4m3_value(tv[j], (w[2 + (j >> 1)] >> (16 * (j & 1))) & 0xFFFFu);
-                        }
-                    }
-                    // a positive second moment stays positive: at least the smallest code
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) tv[j] = r[j] > 0.0f ? fmaxf(tv[j], 0.001953125f) : tv[j];
-                    store_codes(e.m, i, left, cvt_e4m3x2(tm[0], tm[1]) | cvt_e4m3x2(tm[2], tm[3]) << 16);
-                    store_codes(e.v, i, left, cvt_e4m3x2(tv[0], tv[1]) | cvt_e4m3x2(tv[2], tv[3]) << 16);
-                    if (lane == 0) { e.m_scale[b / kBlock] = sm; e.v_scale[b / kBlock] = sv; }
-                } else {
-                    store4(static_cast<float *>(e.m), i, left, m);
-                    store4(static_cast<float *>(e.v), i, left, v);
-                }
-                if constexpr (P_BF16) {
-                    uint32_t bits[4];
-                    if constexpr (SR) {
-                        uint32_t w[4];
-                        philox4x32_10((uint32_t)q, (uint32_t)(q >> 32), tensor, 2u * step + 1u, (uint32_t)c.seed, (uint32_t)(c.seed >> 32), w);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) bits[j] = sr_bf16_bits(p[j], (w[j >> 1] >> (16 * (j & 1))) & 0xFFFFu);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) bits[j] = bf16_bits(p[j]);
-                    }
-                    store4(static_cast<uint16_t *>(e.param), i, left, bits);
-                } else {
-                    store4(static_cast<float *>(e.param), i, left, p);
-                    if (e.param_bf16) {
-                        uint32_t bits[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) bits[j] = bf16_bits(p[j]);
-                        store4(e.param_bf16, i, left, bits);
-                    }
-                }
-            }
+        Chunk k;
+        const int entry = locate<CAP, P_BF16, G_BF16, BITS8>(a, chunk, k);
+        s.keep = (float)(1.0 - (double)s.h.lr * (double)a.e[entry].weight_decay);
+        s.tensor = (uint32_t)(c.first_tensor + entry);
+        const bool full = k.left == kChunk;
+        if constexpr (BITS8) {
+            if (full) run_chunk8<true, P_BF16, G_BF16, SR>(s, k, warp, lane);
+            else run_chunk8<false, P_BF16, G_BF16, SR>(s, k, warp, lane);
+        } else {
+            if (full) run_chunk32<true, P_BF16, G_BF16, SR>(s, k, warp, lane);
+            else run_chunk32<false, P_BF16, G_BF16, SR>(s, k, warp, lane);
         }
     }
 }
@@ -375,7 +525,7 @@ extern "C" int snip_adamw_step(const snip_adamw_tensor_t *ts, int64_t count, con
     if (a->state_bits != 8 && a->state_bits != 32) return SNIP_ERR_ARG;
     if (a->rounding != SNIP_ROUND_NEAREST_EVEN && a->rounding != SNIP_ROUND_STOCHASTIC) return SNIP_ERR_ARG;
     if (!(fabs(a->lr) <= FLT_MAX) || !(a->beta1 >= 0.0 && a->beta1 < 1.0) || !(a->beta2 >= 0.0 && a->beta2 < 1.0)) return SNIP_ERR_ARG;
-    if (!((float)a->eps > 0.0f && a->eps <= FLT_MAX) || (!a->step_device && a->step < 1)) return SNIP_ERR_ARG;
+    if (!((float)a->eps >= FLT_MIN && a->eps <= FLT_MAX) || (!a->step_device && a->step < 1)) return SNIP_ERR_ARG;
     if (count > INT32_MAX) return SNIP_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(a->step_device) & 7u) || (reinterpret_cast<uintptr_t>(a->lr_device) & 3u) || (reinterpret_cast<uintptr_t>(a->grad_scale) & 3u)) return SNIP_ERR_ALIGN;
     for (int64_t i = 0; i < count; ++i) {
@@ -402,7 +552,7 @@ extern "C" int snip_adamw_step(const snip_adamw_tensor_t *ts, int64_t count, con
     c.lr = a->lr; c.beta1 = a->beta1; c.beta2 = a->beta2;
     if (!a->step_device) c.h = hyper(a->lr, a->beta1, a->beta2, a->step);
     c.step_device = a->step_device; c.lr_device = a->lr_device; c.grad_scale = a->grad_scale;
-    c.seed = a->seed;
+    c.k0 = (uint32_t)a->seed; c.k1 = (uint32_t)(a->seed >> 32);
     c.step = (uint32_t)a->step;
     c.b1 = (float)a->beta1; c.omb1 = (float)(1.0 - a->beta1);
     c.b2 = (float)a->beta2; c.omb2 = (float)(1.0 - a->beta2);
