@@ -531,51 +531,70 @@ def _require(ok, what):
         raise ValueError(what)
 
 
-def _same_device(tensors):
-    """Index of the one CUDA device that all of `tensors` (None: not given) are on."""
-    dev = None
-    for t in tensors:
-        if t is not None:
-            _require(t.is_cuda, "tensors have to be on a CUDA device")
-            d = t.get_device()
-            _require(dev is None or d == dev, "tensors have to be on one device")
-            dev = d
+if _device is None:
+    def _device():
+        return torch.cuda.current_device()
+
+
+def _call_on(dev, fn, call, args):
+    """The library's `call(*args, stream)` on the current stream of device `dev`, with `dev` current meanwhile."""
+    if dev == _device():
+        _check(fn, call(*args, _stream()))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn, call(*args, _stream()))
+
+
+# The calls below are short on the device, and their checks are what the host does most of: each asks a tensor for no more than it has to.
+_BF16, _F32, _U8 = torch.bfloat16, torch.float32, torch.uint8
+
+
+def _matrix(t, shape, dev, name):
+    """Checks a bf16 matrix of `shape` on device `dev`; its row stride."""
+    if t.dtype is not _BF16 or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{name}: a bf16 tensor of shape {tuple(shape)} on CUDA device {dev} is wanted")
+    ld, step = t.stride()
+    if step != 1 and shape[1] != 1:
+        raise ValueError(f"{name}: the elements of a row have to be adjacent")
+    return ld if shape[0] > 1 else shape[1]   # a single row's stride says nothing
+
+
+def _vector(t, n, dtype, dev, name):
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous elements of {dtype} on CUDA device {dev} are wanted")
+    return t.data_ptr()
+
+
+def _gain(t, cols, dev):
+    dtype = t.dtype
+    if dtype is not _BF16 and dtype is not _F32 or t.dim() != 1:
+        raise ValueError("gain: a bf16 or float32 vector is wanted")
+    return _vector(t, cols, dtype, dev, "gain"), OUT_BF16 if dtype is _BF16 else OUT_FP32
+
+
+def _cuda_device(t, name):
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name}: a tensor on a CUDA device is wanted")
     return dev
 
 
-def _call_on(dev, fn, call):
-    """call(stream) on device `dev`'s current stream, with `dev` current meanwhile."""
-    if dev is None or dev == torch.cuda.current_device():
-        _check(fn, call(_stream()))
-    else:
-        with torch.cuda.device(dev):
-            _check(fn, call(_stream()))
-
-
-def _matrix(t, shape, name):
-    """Checks a bf16 matrix of `shape`; its row stride."""
-    _require(t.dtype == torch.bfloat16 and t.shape == shape, f"{name}: a bf16 tensor of shape {tuple(shape)} is wanted")
-    rows, cols = shape
-    _require(cols == 1 or t.stride(1) == 1, f"{name}: the elements of a row have to be adjacent")
-    return t.stride(0) if rows > 1 else cols   # a single row's stride says nothing
-
-
-def _vector(t, n, dtypes, name):
-    _require(t.dtype in dtypes and t.numel() == n and t.is_contiguous(), f"{name}: {n} contiguous elements of {' or '.join(map(str, dtypes))} are wanted")
-
-
-def _gain(t, cols):
-    _require(t.dim() == 1, "gain: a vector is wanted")
-    _vector(t, cols, (torch.bfloat16, torch.float32), "gain")
-    return OUT_BF16 if t.dtype == torch.bfloat16 else OUT_FP32
-
-
 _RMSNORM_OUTPUTS = frozenset(("h", "y", "rstd", "codes", "scales", "codes_t", "scales_t"))
+_QUANT = (FMT_FP8_E4M3, FMT_FP4_E2M1)
 
 
 def _code_bytes(rows, cols, fmt):
     """As snip_quantize_sizes, for any number of rows and a multiple of 8 columns."""
     return rows * cols if fmt == FMT_FP8_E4M3 else rows * cols // 2 + (64 if rows % 128 or cols % 128 else 0)
+
+
+def _copy_of(codes, scales, fmt, lines, along, dev, name):
+    """Checks one quantized copy; the two addresses."""
+    if fmt not in _QUANT:
+        raise ValueError(f"{name}: codes are FMT_FP8_E4M3 or FMT_FP4_E2M1")
+    if codes.dtype is not _U8 or codes.numel() < _code_bytes(lines, along, fmt) or codes.get_device() != dev or not codes.is_contiguous():
+        raise ValueError(f"{name}: {_code_bytes(lines, along, fmt)} contiguous bytes on CUDA device {dev} are wanted")
+    return codes.data_ptr(), _vector(scales, -(-along // 128) * lines, _F32, dev, "scales of " + name)
 
 
 def snip_rmsnorm_fwd(x: torch.Tensor, gain: torch.Tensor, eps: float, *, residual=None, fmt=None, fmt_t=None, want_y=None, out=None):
@@ -584,42 +603,54 @@ def snip_rmsnorm_fwd(x: torch.Tensor, gain: torch.Tensor, eps: float, *, residua
     x, residual: bf16 [rows, cols], any row stride that is a multiple of 8.
     Without `out`, buffers are allocated: codes if fmt is FMT_FP8_E4M3 or FMT_FP4_E2M1, codes_t if fmt_t is, y if want_y (default: no codes asked
     for).  With `out`, a dict of such buffers, exactly those that it names are written (out["h"] may be residual or x: the sum in place)."""
-    _require(x.dim() == 2, "x: a matrix is wanted")
-    rows, cols = x.shape
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError("x: a matrix is wanted")
+    rows, cols = shape
+    dev = _cuda_device(x, "x")
     if out is None:
         def empty(n, dtype):
             return torch.empty(n, dtype=dtype, device=x.device)
 
-        quant = (FMT_FP8_E4M3, FMT_FP4_E2M1)
-        _require(fmt in (None, FMT_BF16) + quant and fmt_t in (None, FMT_BF16) + quant, "fmt, fmt_t: FMT_FP8_E4M3, FMT_FP4_E2M1 or None")
-        out = {"h": None if residual is None else empty((rows, cols), torch.bfloat16), "rstd": empty(rows, torch.float32)}
-        if want_y or (want_y is None and fmt not in quant and fmt_t not in quant):
-            out["y"] = empty((rows, cols), torch.bfloat16)
-        if fmt in quant:
-            out["codes"], out["scales"] = empty(_code_bytes(rows, cols, fmt), torch.uint8), empty(-(-cols // 128) * rows, torch.float32)
-        if fmt_t in quant:
-            out["codes_t"], out["scales_t"] = empty(_code_bytes(rows, cols, fmt_t), torch.uint8), empty(-(-rows // 128) * cols, torch.float32)
+        _require(fmt in (None, FMT_BF16) + _QUANT and fmt_t in (None, FMT_BF16) + _QUANT, "fmt, fmt_t: FMT_FP8_E4M3, FMT_FP4_E2M1 or None")
+        out = {"h": None if residual is None else empty((rows, cols), _BF16), "rstd": empty(rows, _F32)}
+        if want_y or (want_y is None and fmt not in _QUANT and fmt_t not in _QUANT):
+            out["y"] = empty((rows, cols), _BF16)
+        if fmt in _QUANT:
+            out["codes"], out["scales"] = empty(_code_bytes(rows, cols, fmt), _U8), empty(-(-cols // 128) * rows, _F32)
+        if fmt_t in _QUANT:
+            out["codes_t"], out["scales_t"] = empty(_code_bytes(rows, cols, fmt_t), _U8), empty(-(-rows // 128) * cols, _F32)
     else:
         _require(want_y is None, "want_y: `out` says what is produced")
-        _require(_RMSNORM_OUTPUTS.issuperset(out), f"out: unknown outputs {sorted(set(out) - _RMSNORM_OUTPUTS)}")
+        if not _RMSNORM_OUTPUTS.issuperset(out):
+            raise ValueError(f"out: unknown outputs {sorted(set(out) - _RMSNORM_OUTPUTS)}")
     get = out.get
     h, y, rstd, codes, scales, codes_t, scales_t = get("h"), get("y"), get("rstd"), get("codes"), get("scales"), get("codes_t"), get("scales_t")
     if residual is None and h is x:
         h = None   # what an earlier call returned for h
-    _require((residual is None) == (h is None), "out: h goes with a residual")
-    a = RmsNorm(_p(x), _p(residual), _p(gain), _p(h), _p(y), _p(rstd), _p(codes), _p(scales), _p(codes_t), _p(scales_t), rows, cols, _matrix(x, x.shape, "x"),
-                0 if residual is None else _matrix(residual, x.shape, "residual"), 0 if h is None else _matrix(h, x.shape, "h"),
-                0 if y is None else _matrix(y, x.shape, "y"), eps, _gain(gain, cols), FMT_BF16 if fmt is None else fmt, FMT_BF16 if fmt_t is None else fmt_t)
+    a = RmsNorm()
+    a.rows, a.cols, a.eps = rows, cols, eps
+    a.ld_x, a.x = _matrix(x, shape, dev, "x"), x.data_ptr()
+    a.gain, a.gain_dtype = _gain(gain, cols, dev)
+    if residual is not None:
+        _require(h is not None, "out: the sum with a residual needs h")
+        a.ld_residual, a.residual = _matrix(residual, shape, dev, "residual"), residual.data_ptr()
+        a.ld_h, a.h = _matrix(h, shape, dev, "h"), h.data_ptr()
+    else:
+        _require(h is None, "out: h goes with a residual")
+    if y is not None:
+        a.ld_y, a.y = _matrix(y, shape, dev, "y"), y.data_ptr()
     if rstd is not None:
-        _vector(rstd, rows, (torch.float32,), "rstd")
-    for c, s, f, lines, along in ((codes, scales, fmt, rows, cols), (codes_t, scales_t, fmt_t, cols, rows)):
-        _require((c is None) == (s is None), "out: codes and scales go together")
-        if c is not None:
-            _require(f in (FMT_FP8_E4M3, FMT_FP4_E2M1), "codes are FMT_FP8_E4M3 or FMT_FP4_E2M1")
-            _require(c.dtype == torch.uint8 and c.is_contiguous() and c.numel() >= _code_bytes(rows, cols, f), "codes: too small, or not bytes")
-            _vector(s, -(-along // 128) * lines, (torch.float32,), "scales")
-    dev = _same_device((x, residual, gain, h, y, rstd, codes, scales, codes_t, scales_t))
-    _call_on(dev, "snip_rmsnorm_fwd", lambda st: _lib.snip_rmsnorm_fwd(ctypes.byref(a), st))
+        a.rstd = _vector(rstd, rows, _F32, dev, "rstd")
+    if (codes is None) != (scales is None) or (codes_t is None) != (scales_t is None):
+        raise ValueError("out: codes and scales go together")
+    if codes is not None:
+        a.codes, a.scales = _copy_of(codes, scales, fmt, rows, cols, dev, "codes")
+        a.fmt = fmt
+    if codes_t is not None:
+        a.codes_t, a.scales_t = _copy_of(codes_t, scales_t, fmt_t, cols, rows, dev, "codes_t")
+        a.fmt_t = fmt_t
+    _call_on(dev, "snip_rmsnorm_fwd", _lib.snip_rmsnorm_fwd, (a,))
     return {"h": x if h is None else h, "y": y, "rstd": rstd, "codes": codes, "scales": scales, "codes_t": codes_t, "scales_t": scales_t}
 
 
@@ -633,25 +664,33 @@ def snip_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd
                      accumulate=False, ws=None):
     """Gradients of the norm: (dx, dgain).  dy, h, dresidual: bf16 [rows, cols]; h, rstd: of the forward call.  dx (bf16) may be dy or dresidual;
     dgain: float32 [cols] (None with want_dgain=False), added to with accumulate."""
-    _require(dy.dim() == 2, "dy: a matrix is wanted")
-    rows, cols = dy.shape
+    shape = dy.shape
+    if len(shape) != 2:
+        raise ValueError("dy: a matrix is wanted")
+    rows, cols = shape
+    dev = _cuda_device(dy, "dy")
     if dx is None:
-        dx = torch.empty((rows, cols), dtype=torch.bfloat16, device=dy.device)
+        dx = torch.empty((rows, cols), dtype=_BF16, device=dy.device)
     if dgain is None and want_dgain:
         _require(not accumulate, "accumulate: needs the dgain to add to")
-        dgain = torch.empty(cols, dtype=torch.float32, device=dy.device)
-    a = RmsNormBwd(_p(dy), _p(h), _p(gain), _p(rstd), _p(dresidual), _p(dx), _p(dgain), rows, cols, _matrix(dy, dy.shape, "dy"), _matrix(h, dy.shape, "h"),
-                   0 if dresidual is None else _matrix(dresidual, dy.shape, "dresidual"), _matrix(dx, dy.shape, "dx"), _gain(gain, cols), int(accumulate))
-    _vector(rstd, rows, (torch.float32,), "rstd")
+        dgain = torch.empty(cols, dtype=_F32, device=dy.device)
+    a = RmsNormBwd()
+    a.rows, a.cols, a.accumulate = rows, cols, 1 if accumulate else 0
+    a.ld_dy, a.dy = _matrix(dy, shape, dev, "dy"), dy.data_ptr()
+    a.ld_h, a.h = _matrix(h, shape, dev, "h"), h.data_ptr()
+    a.ld_dx, a.dx = _matrix(dx, shape, dev, "dx"), dx.data_ptr()
+    if dresidual is not None:
+        a.ld_dresidual, a.dresidual = _matrix(dresidual, shape, dev, "dresidual"), dresidual.data_ptr()
+    a.gain, a.gain_dtype = _gain(gain, cols, dev)
+    a.rstd = _vector(rstd, rows, _F32, dev, "rstd")
+    at, size = None, 0
     if dgain is not None:
-        _vector(dgain, cols, (torch.float32,), "dgain")
+        a.dgain = _vector(dgain, cols, _F32, dev, "dgain")
         if ws is None:
-            ws = torch.empty(snip_rmsnorm_bwd_workspace(rows, cols), dtype=torch.uint8, device=dy.device)
-    if ws is not None:
-        _require(ws.is_contiguous(), "ws: contiguous memory is wanted")
-    dev = _same_device((dy, h, gain, rstd, dresidual, dx, dgain, ws))
-    size = 0 if ws is None else ws.numel() * ws.element_size()
-    _call_on(dev, "snip_rmsnorm_bwd", lambda st: _lib.snip_rmsnorm_bwd(ctypes.byref(a), _p(ws), size, st))
+            ws = torch.empty(snip_rmsnorm_bwd_workspace(rows, cols), dtype=_U8, device=dy.device)
+        size = ws.numel() * ws.element_size()
+        at = _vector(ws, ws.numel(), ws.dtype, dev, "ws")
+    _call_on(dev, "snip_rmsnorm_bwd", _lib.snip_rmsnorm_bwd, (a, at, size))
     return dx, dgain
 
 
@@ -680,7 +719,7 @@ def make_adamw_tensors(params, grads, m, v, *, m_scales=None, v_scales=None, cop
         _require(ts is None or len(ts) == count, f"{name}: one entry per parameter is wanted")
     _require(len(decay) == count, "weight_decay: a number, or one per parameter")
     lists = {name: [None] * count if ts is None else list(ts) for name, ts in lists.items()}
-    device = _same_device([t for ts in lists.values() for t in ts])
+    device = next((_cuda_device(t, "params") for t in lists["params"]), None)
     first = {name: next((t.dtype for t in ts if t is not None), None) for name, ts in lists.items()}
     _require(first["params"] in (None, torch.float32, torch.bfloat16) and first["grads"] in (None, torch.float32, torch.bfloat16), "params, grads: float32 or bf16")
     bits = 8 if first["m"] == torch.uint8 else 32
@@ -700,8 +739,7 @@ def make_adamw_tensors(params, grads, m, v, *, m_scales=None, v_scales=None, cop
             t = ts[i]
             _require((t is not None) == (name in wanted), f"{name}[{i}]: {'missing' if t is None else 'not wanted'}")
             if t is not None:
-                _vector(t, *wanted[name][:1], (wanted[name][1],), f"{name}[{i}]")
-                row[name] = t.data_ptr()
+                row[name] = _vector(t, *wanted[name], device, f"{name}[{i}]")
                 if t.numel() and name != "grads":
                     written.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()))
         table[i] = AdamwTensor(row["params"], row["grads"], row["m"], row["v"], row.get("m_scales"), row.get("v_scales"), row.get("copies"), n, decay[i], 0)
@@ -721,15 +759,15 @@ def snip_adamw_step(tensors: AdamwTensors, lr, beta1: float, beta2: float, eps: 
     tensor with one element (both are then read when the step runs, also by each replay of a captured graph).  grad_scale: None, or a float32 CUDA tensor with one
     element by which every gradient is multiplied."""
     lr_dev, step_dev = lr if isinstance(lr, torch.Tensor) else None, step if isinstance(step, torch.Tensor) else None
-    for t, dtype, name in ((lr_dev, torch.float32, "lr"), (step_dev, torch.int64, "step"), (grad_scale, torch.float32, "grad_scale")):
+    if tensors.count == 0:
+        return
+    for t, dtype, name in ((lr_dev, _F32, "lr"), (step_dev, torch.int64, "step"), (grad_scale, _F32, "grad_scale")):
         if t is not None:
-            _vector(t, 1, (dtype,), name)
-            _require(t.is_cuda and (tensors.device is None or t.get_device() == tensors.device), f"{name}: not on the tensors' device")
+            _vector(t, 1, dtype, tensors.device, name)
     _require(0 <= seed < 1 << 64, "seed: 64 bits")
     a = Adamw(0.0 if lr_dev is not None else lr, beta1, beta2, eps, 0 if step_dev is not None else step, _p(step_dev), _p(lr_dev), _p(grad_scale), seed,
               tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, rounding)
-    if tensors.count:
-        _call_on(tensors.device, "snip_adamw_step", lambda st: _lib.snip_adamw_step(tensors.table, tensors.count, ctypes.byref(a), st))
+    _call_on(tensors.device, "snip_adamw_step", _lib.snip_adamw_step, (tensors.table, tensors.count, a))
 
 
 def snip_loss_divergence(grad_x_norm, err_x_norm, M, K, grad_w_norm, err_w_norm, N, loss) -> float:

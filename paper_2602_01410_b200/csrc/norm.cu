@@ -11,6 +11,7 @@
 #include <cuda_bf16.h>
 #include <float.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "common.cuh"
@@ -33,7 +34,7 @@ struct NormArgs {
     float *scales;
     int64_t ld_x, ld_residual, ld_h, ld_y;
     int32_t rows, cols;
-    int gain_f32, fmt;
+    int gain_f32;
     float eps, inv_cols;
 };
 
@@ -49,40 +50,72 @@ struct NormBwdArgs {
     float inv_cols;
 };
 
-// 16 bytes that this kernel reads once (they may be overwritten in place afterwards: not the read-only path)
-__device__ __forceinline__ uint4 load_once(const uint16_t *p)
+// Eight neighbouring elements as four pairs.
+struct Eight {
+    float2 p[4];
+};
+__device__ __forceinline__ float2 splat(float x) { return make_float2(x, x); }
+__device__ __forceinline__ Eight unpack8(const uint4 &v)
 {
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
+    return {{make_float2(bf16lo(v.x), bf16hi(v.x)), make_float2(bf16lo(v.y), bf16hi(v.y)), make_float2(bf16lo(v.z), bf16hi(v.z)), make_float2(bf16lo(v.w), bf16hi(v.w))}};
 }
-
-__device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
-{
-    f[0] = bf16lo(v.x); f[1] = bf16hi(v.x); f[2] = bf16lo(v.y); f[3] = bf16hi(v.y);
-    f[4] = bf16lo(v.z); f[5] = bf16hi(v.z); f[6] = bf16lo(v.w); f[7] = bf16hi(v.w);
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+__device__ __forceinline__ uint32_t pack2(const float2 f)
 {
     uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(f.y), "f"(f.x));
     return r;
 }
-__device__ __forceinline__ uint4 pack8(const float (&f)[8])
+__device__ __forceinline__ uint4 pack8(const Eight &e) { return make_uint4(pack2(e.p[0]), pack2(e.p[1]), pack2(e.p[2]), pack2(e.p[3])); }
+__device__ __forceinline__ Eight zeros8() { return {{splat(0.0f), splat(0.0f), splat(0.0f), splat(0.0f)}}; }
+
+// (h rstd) gain, each product rounded: what every form of the forward pass quantizes
+__device__ __forceinline__ Eight scaled8(const Eight &h, float rstd, const Eight &gain)
 {
-    return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+    Eight y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y.p[i] = __fmul2_rn(__fmul2_rn(h.p[i], splat(rstd)), gain.p[i]);
+    return y;
+}
+__device__ __forceinline__ float most8(const Eight &y)
+{
+    float m = fmaxf(fabsf(y.p[0].x), fabsf(y.p[0].y));
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = fmaxf(fmaxf(m, fabsf(y.p[i].x)), fabsf(y.p[i].y));
+    return m;
 }
 
-__device__ __forceinline__ void load_gain8(const void *gain, int f32, int col, float (&g)[8])
+// Codes of eight neighbouring elements under one scale.
+template <int FMT>
+__device__ __forceinline__ void store_codes8(uint8_t *codes, int64_t at, const Eight &y, float s)
 {
-    if (f32) {
-        const float4 a = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(gain) + col));
-        const float4 b = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(gain) + col) + 1);
-        g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w; g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
+    float2 t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = __fmul2_rn(y.p[i], splat(s));
+    if constexpr (FMT == SNIP_FMT_FP8_E4M3) {
+        *reinterpret_cast<uint2 *>(codes + at) = make_uint2(__byte_perm(cvt_e4m3x2(t[0].x, t[0].y), cvt_e4m3x2(t[1].x, t[1].y), 0x5410),
+                                                            __byte_perm(cvt_e4m3x2(t[2].x, t[2].y), cvt_e4m3x2(t[3].x, t[3].y), 0x5410));
     } else {
-        unpack8(__ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(gain) + col)), g);
+        *reinterpret_cast<uint32_t *>(codes + at / 2) = cvt_e2m1x2(t[0].x, t[0].y) | cvt_e2m1x2(t[1].x, t[1].y) << 8 | cvt_e2m1x2(t[2].x, t[2].y) << 16 |
+                                                        cvt_e2m1x2(t[3].x, t[3].y) << 24;
     }
 }
+
+__device__ __forceinline__ Eight load_gain8(const void *gain, int f32, int col)
+{
+    if (!f32) return unpack8(__ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(gain) + col)));
+    const float4 a = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(gain) + col));
+    const float4 b = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(gain) + col) + 1);
+    return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
+}
+
+// 16 bytes into this thread's own slot of shared memory (read back by itself: nothing to wait for but its own copies), or zeros.
+__device__ __forceinline__ void copy_async(uint4 *slot, const uint16_t *src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(slot)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Sum over the WPR warps of a row group, in a fixed order; the same value in every thread.  `slots` (one float per warp of the CTA) is free again
 // when all threads have come past the next call's barrier: callers alternate between two sets.
@@ -106,98 +139,103 @@ __device__ __forceinline__ float group_sum(float v, float *slots)
 __host__ __device__ constexpr int cta_threads(int wpr) { return wpr < 8 ? 256 : 32 * wpr; }
 __host__ __device__ constexpr int groups_per_cta(int wpr) { return cta_threads(wpr) / (32 * wpr); }
 
+// Rows on their way: a thread's slots for kStages rows of N arrays of V vectors.
+template <int WPR, int V, int N>
+struct Ring {
+    static constexpr int kRowBytes = N * V * cta_threads(WPR) * 16;
+    static constexpr int kStages = kRowBytes > 100 * 1024 ? 1 : kRowBytes > 24 * 1024 ? 2 : kRowBytes > 12 * 1024 ? 3 : 4;
+    static constexpr int kBytes = kStages * kRowBytes;
+    static_assert(kBytes <= 224 * 1024, "an SM has 227 KB");
+    uint4 *base;
+    __device__ __forceinline__ uint4 *slot(int stage, int array, int k) const { return base + ((stage * N + array) * V + k) * cta_threads(WPR) + threadIdx.x; }
+};
+
 // WPR warps per row, V vectors of eight elements per thread: vector k of thread t of the group starts at column 8 (t + k 32 WPR), so
-// that 16 neighbouring threads hold a 128-long tile.
-template <int WPR, int V, bool RES>
+// that 16 neighbouring threads hold a 128-long tile.  FMT: format of the row-tile codes, BF16 for none.
+template <int WPR, int V, bool RES, int FMT>
 __global__ void __launch_bounds__(cta_threads(WPR)) rmsnorm_kernel(const NormArgs a)
 {
+    extern __shared__ __align__(16) uint8_t raw[];
     __shared__ float slots[2][32];
+    using R = Ring<WPR, V, RES ? 2 : 1>;
+    const R ring = {reinterpret_cast<uint4 *>(raw)};
     constexpr int kGroups = groups_per_cta(WPR);
-    const int t = threadIdx.x % (32 * WPR);
+    const int t = threadIdx.x % (32 * WPR), group = threadIdx.x / (32 * WPR);
     const int64_t step = (int64_t)gridDim.x * kGroups;
-    float gain[V][8];
-    bool in[V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-        const int col = 8 * (t + k * 32 * WPR);
-        in[k] = col < a.cols;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) gain[k][i] = 0.0f;
-        if (in[k]) load_gain8(a.gain, a.gain_f32, col, gain[k]);
-    }
-    uint4 x[V], r[V];
-    auto fetch = [&](int64_t row) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            x[k] = make_uint4(0, 0, 0, 0);
-            if (RES) r[k] = make_uint4(0, 0, 0, 0);
-            if (in[k] && row < a.rows) {
-                const int col = 8 * (t + k * 32 * WPR);
-                x[k] = load_once(a.x + row * a.ld_x + col);
-                if (RES) r[k] = load_once(a.residual + row * a.ld_residual + col);
-            }
-        }
-    };
-    // all groups of a CTA take the same number of turns: rows behind the last are zeros that nothing is written for
-    const int64_t first = (int64_t)blockIdx.x * kGroups;
-    const int group = threadIdx.x / (32 * WPR);
-    fetch(first + group);
-    int parity = 0;
-    for (int64_t base = first; base < a.rows; base += step, parity ^= 1) {
-        const int64_t row = base + group;
-        float h[V][8];
-        float sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            unpack8(x[k], h[k]);
-            if (RES) {
-                float q[8];
-                unpack8(r[k], q);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[k][i] += q[i];
-                const uint4 packed = pack8(h[k]);
-                if (in[k] && row < a.rows) *reinterpret_cast<uint4 *>(a.h + row * a.ld_h + 8 * (t + k * 32 * WPR)) = packed;
-                unpack8(packed, h[k]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(h[k][i], h[k][i], sum);
-        }
-        fetch(row + step);
-        sum = group_sum<WPR>(sum, slots[parity]);
-        const float rstd = __frcp_rn(__fsqrt_rn(fmaf(sum, a.inv_cols, a.eps)));
-        if (t == 0 && a.rstd && row < a.rows) a.rstd[row] = rstd;
-        if (!a.y && !a.codes) continue;
+    auto fetch = [&](int stage, int64_t row) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int col = 8 * (t + k * 32 * WPR);
-            const bool ok = in[k] && row < a.rows;
+            const bool there = col < a.cols && row < a.rows;
+            copy_async(ring.slot(stage, 0, k), a.x + (there ? row * a.ld_x + col : 0), there);
+            if (RES) copy_async(ring.slot(stage, 1, k), a.residual + (there ? row * a.ld_residual + col : 0), there);
+        }
+        copies_commit();
+    };
+    int64_t row = (int64_t)blockIdx.x * kGroups + group;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[k][i] = __fmul_rn(__fmul_rn(h[k][i], rstd), gain[k][i]);
-            if (a.y && ok) *reinterpret_cast<uint4 *>(a.y + row * a.ld_y + col) = pack8(h[k]);
-            if (a.codes) {
-                float most = 0.0f;
+    for (int i = 0; i < R::kStages - 1; ++i) fetch(i, row + i * step);
+    // of the widest rows neither the gain nor the row in binary32 stays in registers
+    constexpr bool kWide = V > 2;
+    Eight gain[kWide ? 1 : V];
+    if constexpr (!kWide) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(h[k][i]));
+        for (int k = 0; k < V; ++k) {
+            const int col = 8 * (t + k * 32 * WPR);
+            gain[k] = col < a.cols ? load_gain8(a.gain, a.gain_f32, col) : zeros8();
+        }
+    }
+    int parity = 0, stage = 0;
+    // all groups of a CTA take the same number of turns: rows behind the last are zeros that nothing is written for
+    for (int64_t base = (int64_t)blockIdx.x * kGroups; base < a.rows; base += step, row += step, parity ^= 1) {
+        fetch(stage == 0 ? R::kStages - 1 : stage - 1, row + (R::kStages - 1) * step);
+        copies_wait<R::kStages - 1>();
+        Eight h[kWide ? 1 : V];
+        uint4 packed[V];
+        float2 sum = splat(0.0f);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int col = 8 * (t + k * 32 * WPR);
+            packed[k] = *ring.slot(stage, 0, k);
+            Eight e = unpack8(packed[k]);
+            if (RES) {
+                const Eight q = unpack8(*ring.slot(stage, 1, k));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e.p[i] = __fadd2_rn(e.p[i], q.p[i]);
+                packed[k] = pack8(e);
+                if (col < a.cols && row < a.rows) *reinterpret_cast<uint4 *>(a.h + row * a.ld_h + col) = packed[k];
+                e = unpack8(packed[k]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum = __ffma2_rn(e.p[i], e.p[i], sum);
+            if constexpr (!kWide) h[k] = e;
+        }
+        stage = stage == R::kStages - 1 ? 0 : stage + 1;
+        const float total = group_sum<WPR>(sum.x + sum.y, slots[parity]);
+        const float rstd = __frcp_rn(__fsqrt_rn(fmaf(total, a.inv_cols, a.eps)));
+        if (t == 0 && a.rstd && row < a.rows) a.rstd[row] = rstd;
+        if (FMT == SNIP_FMT_BF16 && !a.y) continue;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int col = 8 * (t + k * 32 * WPR);
+            const bool ok = col < a.cols && row < a.rows;
+            Eight y;
+            if constexpr (kWide) y = scaled8(unpack8(packed[k]), rstd, col < a.cols ? load_gain8(a.gain, a.gain_f32, col) : zeros8());
+            else y = scaled8(h[k], rstd, gain[k]);
+            if (a.y && ok) *reinterpret_cast<uint4 *>(a.y + row * a.ld_y + col) = pack8(y);
+            if constexpr (FMT != SNIP_FMT_BF16) {
+                float most = most8(y);
 #pragma unroll
                 for (int off = 8; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, off));
-                const bool fp8 = a.fmt == SNIP_FMT_FP8_E4M3;
-                const float s = fp8 ? tile_scale<SNIP_FMT_FP8_E4M3>(most, 0) : tile_scale<SNIP_FMT_FP4_E2M1>(most, 0);
+                const float s = tile_scale<FMT>(most, 0);
                 if (ok) {
                     if ((t & 15) == 0) a.scales[(int64_t)(col >> 7) * a.rows + row] = s;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) h[k][i] *= s;
-                    const int64_t at = row * a.cols + col;
-                    if (fp8) {
-                        *reinterpret_cast<uint2 *>(a.codes + at) = make_uint2(cvt_e4m3x2(h[k][0], h[k][1]) | cvt_e4m3x2(h[k][2], h[k][3]) << 16,
-                                                                              cvt_e4m3x2(h[k][4], h[k][5]) | cvt_e4m3x2(h[k][6], h[k][7]) << 16);
-                    } else {
-                        *reinterpret_cast<uint32_t *>(a.codes + at / 2) = cvt_e2m1x2(h[k][0], h[k][1]) | cvt_e2m1x2(h[k][2], h[k][3]) << 8 |
-                                                                          cvt_e2m1x2(h[k][4], h[k][5]) << 16 | cvt_e2m1x2(h[k][6], h[k][7]) << 24;
-                    }
+                    store_codes8<FMT>(a.codes, row * a.cols + col, y, s);
                 }
             }
         }
     }
+    copies_wait<0>();
 }
 
 // Both quantized copies of y from h and rstd: 128x128 tiles, a thread owns 8x8 elements of one (dimensions are multiples of 64: all of
@@ -212,7 +250,7 @@ struct NormDualArgs {
     int64_t ld;
     int32_t rows, cols, tiles_c;
     int64_t tiles;
-    int gain_f32, fmt, fmt_t;
+    int gain_f32;
 };
 constexpr int kTile = 128;
 constexpr int kDualThreads = 256;
@@ -226,6 +264,8 @@ struct DualShared {
     float row_scale[kTile];
 };
 
+// FMT: format of the row-tile codes (BF16: none), FMT_T: of the transposed ones.
+template <int FMT, int FMT_T>
 __global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(const NormDualArgs a)
 {
     extern __shared__ __align__(128) uint8_t raw[];
@@ -235,57 +275,57 @@ __global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(c
         const int64_t row = tile / a.tiles_c * kTile + 8 * ty, col = tile % a.tiles_c * kTile + 8 * tx;
         const bool ok = tile < a.tiles && row < a.rows && col < a.cols;
         const uint16_t *p = a.h + (ok ? row * a.ld + col : 0);
-        const int bytes = ok ? 16 : 0;   // 0: the slot is filled with zeros, nothing is read
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(&m.slot[i][tid])), "l"(p + (ok ? i * a.ld : 0)), "r"(bytes) : "memory");
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        for (int i = 0; i < 8; ++i) copy_async(&m.slot[i][tid], p + (ok ? i * a.ld : 0), ok);
+        copies_commit();
     };
     fetch(blockIdx.x);
     for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const int row0 = (int)(tile / a.tiles_c) * kTile + 8 * ty, col0 = (int)(tile % a.tiles_c) * kTile + 8 * tx;
+        const int tr = (int)(tile / a.tiles_c), tc = (int)(tile % a.tiles_c);
+        const int row0 = tr * kTile + 8 * ty, col0 = tc * kTile + 8 * tx;
         const bool ok = row0 < a.rows && col0 < a.cols;
-        float gain[8], rstd[8];
+        Eight gain = zeros8();
+        float rstd[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) gain[i] = rstd[i] = 0.0f;
+        for (int i = 0; i < 8; ++i) rstd[i] = 0.0f;
         if (ok) {
-            load_gain8(a.gain, a.gain_f32, col0, gain);
+            gain = load_gain8(a.gain, a.gain_f32, col0);
             const float4 p = __ldcg(reinterpret_cast<const float4 *>(a.rstd + row0)), q = __ldcg(reinterpret_cast<const float4 *>(a.rstd + row0) + 1);
             rstd[0] = p.x; rstd[1] = p.y; rstd[2] = p.z; rstd[3] = p.w; rstd[4] = q.x; rstd[5] = q.y; rstd[6] = q.z; rstd[7] = q.w;
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        copies_wait<0>();
         float rmax[8], cmax[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) cmax[i] = 0.0f;
 #pragma unroll
-        for (int p = 0; p < 8; ++p) {
-            float f[8];
-            unpack8(m.slot[p][tid], f);
-            rmax[p] = 0.0f;
+        for (int p = 0; p < 8; p += 2) {
+            const Eight y0 = scaled8(unpack8(m.slot[p][tid]), rstd[p], gain), y1 = scaled8(unpack8(m.slot[p + 1][tid]), rstd[p + 1], gain);
+            rmax[p] = most8(y0);
+            rmax[p + 1] = most8(y1);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float v = fabsf(__fmul_rn(__fmul_rn(f[i], rstd[p]), gain[i]));
-                rmax[p] = fmaxf(rmax[p], v);
-                cmax[i] = fmaxf(cmax[i], v);
+            for (int i = 0; i < 4; ++i) {
+                cmax[2 * i] = fmaxf(fmaxf(cmax[2 * i], fabsf(y0.p[i].x)), fabsf(y1.p[i].x));
+                cmax[2 * i + 1] = fmaxf(fmaxf(cmax[2 * i + 1], fabsf(y0.p[i].y)), fabsf(y1.p[i].y));
             }
         }
-        // rows: each step halves the number of rows a lane still looks after; lanes 2 q and 2 q + 1 of a half-warp end with row q's maximum
+        if constexpr (FMT != SNIP_FMT_BF16) {
+            // rows: each step halves the number of rows a lane still looks after; lanes 2 q and 2 q + 1 of a half-warp end with row q's maximum
 #pragma unroll
-        for (int w = 4, off = 8; w > 0; w >>= 1, off >>= 1) {
-            const bool upper = (lane & off) != 0;
+            for (int w = 4, off = 8; w > 0; w >>= 1, off >>= 1) {
+                const bool upper = (lane & off) != 0;
 #pragma unroll
-            for (int i = 0; i < w; ++i) {
-                const float give = upper ? rmax[i] : rmax[i + w], keep = upper ? rmax[i + w] : rmax[i];
-                rmax[i] = fmaxf(keep, __shfl_xor_sync(0xFFFFFFFFu, give, off));
+                for (int i = 0; i < w; ++i) {
+                    const float give = upper ? rmax[i] : rmax[i + w], keep = upper ? rmax[i + w] : rmax[i];
+                    rmax[i] = fmaxf(keep, __shfl_xor_sync(0xFFFFFFFFu, give, off));
+                }
             }
-        }
-        rmax[0] = fmaxf(rmax[0], __shfl_xor_sync(0xFFFFFFFFu, rmax[0], 1));
-        if (a.codes && (lane & 1) == 0) {
-            const float s = a.fmt == SNIP_FMT_FP8_E4M3 ? tile_scale<SNIP_FMT_FP8_E4M3>(rmax[0], 0) : tile_scale<SNIP_FMT_FP4_E2M1>(rmax[0], 0);
-            const int q = (lane >> 1) & 7, r = 8 * ty + q;
-            m.row_scale[r] = s;
-            const int64_t row = tile / a.tiles_c * kTile + r;
-            if (row < a.rows) a.scales[tile % a.tiles_c * a.rows + row] = s;
+            rmax[0] = fmaxf(rmax[0], __shfl_xor_sync(0xFFFFFFFFu, rmax[0], 1));
+            if ((lane & 1) == 0) {
+                const float s = tile_scale<FMT>(rmax[0], 0);
+                const int r = 8 * ty + ((lane >> 1) & 7), row = tr * kTile + r;
+                m.row_scale[r] = s;
+                if (row < a.rows) a.scales[(int64_t)tc * a.rows + row] = s;
+            }
         }
         // columns
 #pragma unroll
@@ -299,154 +339,170 @@ __global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(c
             float v = m.col_max[0][tid];
 #pragma unroll
             for (int w = 1; w < 8; ++w) v = fmaxf(v, m.col_max[w][tid]);
-            const float s = a.fmt_t == SNIP_FMT_FP8_E4M3 ? tile_scale<SNIP_FMT_FP8_E4M3>(v, 0) : tile_scale<SNIP_FMT_FP4_E2M1>(v, 0);
+            const float s = tile_scale<FMT_T>(v, 0);
             m.col_scale[tid] = s;
-            const int64_t col = tile % a.tiles_c * kTile + tid;
-            if (col < a.cols) a.scales_t[tile / a.tiles_c * a.cols + col] = s;
+            const int col = tc * kTile + tid;
+            if (col < a.cols) a.scales_t[(int64_t)tr * a.cols + col] = s;
         }
         __syncthreads();
-        float cs[8];
+        Eight cs;
         {
             const float4 p = *reinterpret_cast<const float4 *>(&m.col_scale[8 * tx]), q = *reinterpret_cast<const float4 *>(&m.col_scale[8 * tx + 4]);
-            cs[0] = p.x; cs[1] = p.y; cs[2] = p.z; cs[3] = p.w; cs[4] = q.x; cs[5] = q.y; cs[6] = q.z; cs[7] = q.w;
+            cs = {{make_float2(p.x, p.y), make_float2(p.z, p.w), make_float2(q.x, q.y), make_float2(q.z, q.w)}};
         }
-        const bool fp8 = a.fmt == SNIP_FMT_FP8_E4M3, fp8_t = a.fmt_t == SNIP_FMT_FP8_E4M3;
         uint32_t ct[8][2];   // column i: codes of its eight rows (FP4: the first word)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ct[i][0] = ct[i][1] = 0u;
+        for (int p = 0; p < 8; p += 4) {
+            uint32_t part[2][8];
 #pragma unroll
-        for (int p = 0; p < 8; p += 2) {
-            float y[2][8];
+            for (int e = 0; e < 4; e += 2) {
+                Eight y[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                unpack8(m.slot[p + e][tid], y[e]);
+                for (int f = 0; f < 2; ++f) {
+                    const int r = p + e + f;
+                    y[f] = scaled8(unpack8(m.slot[r][tid]), rstd[r], gain);
+                    if constexpr (FMT != SNIP_FMT_BF16)
+                        if (ok) store_codes8<FMT>(a.codes, (int64_t)(row0 + r) * a.cols + col0, y[f], m.row_scale[8 * ty + r]);
+                }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[e][i] = __fmul_rn(__fmul_rn(y[e][i], rstd[p + e]), gain[i]);
-                if (a.codes && ok) {
-                    const float s = m.row_scale[8 * ty + p + e];
-                    float z[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) z[i] = y[e][i] * s;
-                    const int64_t at = (int64_t)(row0 + p + e) * a.cols + col0;
-                    if (fp8) *reinterpret_cast<uint2 *>(a.codes + at) = make_uint2(cvt_e4m3x2(z[0], z[1]) | cvt_e4m3x2(z[2], z[3]) << 16, cvt_e4m3x2(z[4], z[5]) | cvt_e4m3x2(z[6], z[7]) << 16);
-                    else *reinterpret_cast<uint32_t *>(a.codes + at / 2) = cvt_e2m1x2(z[0], z[1]) | cvt_e2m1x2(z[2], z[3]) << 8 | cvt_e2m1x2(z[4], z[5]) << 16 | cvt_e2m1x2(z[6], z[7]) << 24;
+                for (int i = 0; i < 4; ++i) {
+                    const float2 t0 = __fmul2_rn(y[0].p[i], cs.p[i]), t1 = __fmul2_rn(y[1].p[i], cs.p[i]);
+                    if constexpr (FMT_T == SNIP_FMT_FP8_E4M3) {
+                        part[e >> 1][2 * i] = cvt_e4m3x2(t0.x, t1.x);
+                        part[e >> 1][2 * i + 1] = cvt_e4m3x2(t0.y, t1.y);
+                    } else {
+                        part[e >> 1][2 * i] = cvt_e2m1x2(t0.x, t1.x);
+                        part[e >> 1][2 * i + 1] = cvt_e2m1x2(t0.y, t1.y);
+                    }
                 }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (fp8_t) ct[i][p >> 2] |= cvt_e4m3x2(y[0][i] * cs[i], y[1][i] * cs[i]) << (8 * (p & 3));
-                else ct[i][0] |= cvt_e2m1x2(y[0][i] * cs[i], y[1][i] * cs[i]) << (4 * p);
+                if constexpr (FMT_T == SNIP_FMT_FP8_E4M3) ct[i][p >> 2] = __byte_perm(part[0][i], part[1][i], 0x5410);
+                else ct[i][p >> 2] = __byte_perm(part[0][i], part[1][i], 0x0040);   // two bytes
             }
         }
         fetch(tile + gridDim.x);   // the slot has been read
         // transposed codes: line = column of the tile, 128 (64) bytes each; 16-byte pieces swizzled by the line so that neither side conflicts
-        if (fp8_t) {
+        constexpr bool kFp8T = FMT_T == SNIP_FMT_FP8_E4M3;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int line = 8 * tx + i, piece = (ty >> 1) ^ (tx & 7);
-                *reinterpret_cast<uint2 *>(&m.stage[line * 128 + piece * 16 + (ty & 1) * 8]) = make_uint2(ct[i][0], ct[i][1]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int line = 8 * tx + i, piece = (ty >> 2) ^ (tx & 3);
-                *reinterpret_cast<uint32_t *>(&m.stage[line * 64 + piece * 16 + (ty & 3) * 4]) = ct[i][0];
-            }
+        for (int i = 0; i < 8; ++i) {
+            const int line = 8 * tx + i;
+            if constexpr (kFp8T) *reinterpret_cast<uint2 *>(&m.stage[line * 128 + ((ty >> 1) ^ (tx & 7)) * 16 + (ty & 1) * 8]) = make_uint2(ct[i][0], ct[i][1]);
+            else *reinterpret_cast<uint32_t *>(&m.stage[line * 64 + ((ty >> 2) ^ (tx & 3)) * 16 + (ty & 3) * 4]) = __byte_perm(ct[i][0], ct[i][1], 0x5410);
         }
         __syncthreads();
-        const int64_t r0 = tile / a.tiles_c * kTile, c0 = tile % a.tiles_c * kTile;
-        const int per_line = fp8_t ? 8 : 4, rows_per_piece = fp8_t ? 16 : 32;
-        for (int j = tid; j < kTile * per_line; j += kDualThreads) {
-            const int line = j / per_line, piece = j % per_line;
-            const int64_t row = r0 + piece * rows_per_piece;
-            if (c0 + line >= a.cols || row >= a.rows) continue;
-            const int at = fp8_t ? line * 128 + ((piece ^ ((line >> 3) & 7)) * 16) : line * 64 + ((piece ^ ((line >> 3) & 3)) * 16);
-            const int64_t elem = (c0 + line) * a.rows + row;
-            *reinterpret_cast<uint4 *>(a.codes_t + (fp8_t ? elem : elem / 2)) = *reinterpret_cast<const uint4 *>(&m.stage[at]);
+        constexpr int kPieces = kFp8T ? 8 : 4, kRows = kFp8T ? 16 : 32;   // 16-byte pieces of a line, rows in one
+#pragma unroll
+        for (int j = 0; j < kTile * kPieces / kDualThreads; ++j) {
+            const int line = (j * kDualThreads + tid) / kPieces, piece = tid % kPieces;
+            const int row = tr * kTile + piece * kRows, col = tc * kTile + line;
+            if (col >= a.cols || row >= a.rows) continue;
+            const int64_t elem = (int64_t)col * a.rows + row;
+            *reinterpret_cast<uint4 *>(a.codes_t + (kFp8T ? elem : elem / 2)) =
+                *reinterpret_cast<const uint4 *>(&m.stage[line * (16 * kPieces) + (piece ^ ((line >> 3) & (kPieces - 1))) * 16]);
         }
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    copies_wait<0>();
 }
 
 template <int WPR, int V, bool RES>
 __global__ void __launch_bounds__(cta_threads(WPR)) rmsnorm_bwd_kernel(const NormBwdArgs a)
 {
+    extern __shared__ __align__(16) uint8_t raw[];
     __shared__ float slots[2][32];
+    using R = Ring<WPR, V, RES ? 3 : 2>;
+    const R ring = {reinterpret_cast<uint4 *>(raw)};
     constexpr int kGroups = groups_per_cta(WPR);
     const int t = threadIdx.x % (32 * WPR), group = threadIdx.x / (32 * WPR);
     const int64_t step = (int64_t)gridDim.x * kGroups, first = (int64_t)blockIdx.x * kGroups;
-    float gain[V][8], dgain[V][8];
-    bool in[V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-        const int col = 8 * (t + k * 32 * WPR);
-        in[k] = col < a.cols;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) gain[k][i] = dgain[k][i] = 0.0f;
-        if (in[k]) load_gain8(a.gain, a.gain_f32, col, gain[k]);
-    }
-    uint4 dy[V], h[V], d[V];
-    float rstd = 0.0f;
-    auto fetch = [&](int64_t row) {
-        const bool any = row < a.rows;
-        if (any) rstd = __ldg(a.rstd + row);
+    auto fetch = [&](int stage, int64_t row) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            dy[k] = h[k] = make_uint4(0, 0, 0, 0);
-            if (RES) d[k] = make_uint4(0, 0, 0, 0);
-            if (in[k] && any) {
-                const int col = 8 * (t + k * 32 * WPR);
-                dy[k] = load_once(a.dy + row * a.ld_dy + col);
-                h[k] = load_once(a.h + row * a.ld_h + col);
-                if (RES) d[k] = load_once(a.dresidual + row * a.ld_dresidual + col);
-            }
+            const int col = 8 * (t + k * 32 * WPR);
+            const bool there = col < a.cols && row < a.rows;
+            copy_async(ring.slot(stage, 0, k), a.dy + (there ? row * a.ld_dy + col : 0), there);
+            copy_async(ring.slot(stage, 1, k), a.h + (there ? row * a.ld_h + col : 0), there);
+            if (RES) copy_async(ring.slot(stage, 2, k), a.dresidual + (there ? row * a.ld_dresidual + col : 0), there);
         }
+        copies_commit();
     };
-    fetch(first + group);
-    int parity = 0;
-    for (int64_t base = first; base < a.rows; base += step, parity ^= 1) {
-        const int64_t row = base + group;
-        float g[V][8], u[V][8];   // dy gain, h rstd
-        uint4 res[V];
-        float dot = 0.0f;
+    int64_t row = first + group;
+#pragma unroll
+    for (int i = 0; i < R::kStages - 1; ++i) fetch(i, row + i * step);
+    // of the widest rows neither the gain nor the products stay in registers
+    constexpr bool kWide = V > 2;
+    auto gain_of = [&](int k) {
+        const int col = 8 * (t + k * 32 * WPR);
+        return col < a.cols ? load_gain8(a.gain, a.gain_f32, col) : zeros8();
+    };
+    Eight gain[kWide ? 1 : V], dgain[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        if constexpr (!kWide) gain[k] = gain_of(k);
+        dgain[k] = zeros8();
+    }
+    float rstd = row < a.rows ? __ldg(a.rstd + row) : 0.0f;
+    int parity = 0, stage = 0;
+    for (int64_t base = first; base < a.rows; base += step, row += step, parity ^= 1) {
+        fetch(stage == 0 ? R::kStages - 1 : stage - 1, row + (R::kStages - 1) * step);
+        copies_wait<R::kStages - 1>();
+        Eight g[kWide ? 1 : V], u[kWide ? 1 : V];   // dy gain, h rstd
+        float2 dot = splat(0.0f);
         const float r = rstd;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            unpack8(dy[k], g[k]);
-            unpack8(h[k], u[k]);
-            if (RES) res[k] = d[k];
+            Eight &gk = g[kWide ? 0 : k], &uk = u[kWide ? 0 : k];
+            gk = unpack8(*ring.slot(stage, 0, k));
+            uk = unpack8(*ring.slot(stage, 1, k));
+            const Eight w = kWide ? gain_of(k) : gain[kWide ? 0 : k];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                u[k][i] *= r;
-                dgain[k][i] = fmaf(g[k][i], u[k][i], dgain[k][i]);
-                g[k][i] *= gain[k][i];
-                dot = fmaf(g[k][i], u[k][i], dot);
+            for (int i = 0; i < 4; ++i) {
+                uk.p[i] = __fmul2_rn(uk.p[i], splat(r));
+                dgain[k].p[i] = __ffma2_rn(gk.p[i], uk.p[i], dgain[k].p[i]);
+                gk.p[i] = __fmul2_rn(gk.p[i], w.p[i]);
+                dot = __ffma2_rn(gk.p[i], uk.p[i], dot);
             }
         }
-        fetch(row + step);
-        const float c = group_sum<WPR>(dot, slots[parity]) * a.inv_cols;
+        if (row + step < a.rows) rstd = __ldg(a.rstd + row + step);
+        const float c = group_sum<WPR>(dot.x + dot.y, slots[parity]) * -a.inv_cols;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            if (!in[k] || row >= a.rows) continue;
-            float q[8];
-            if (RES) unpack8(res[k], q);
+            const int col = 8 * (t + k * 32 * WPR);
+            if (col >= a.cols || row >= a.rows) continue;
+            Eight q;
+            if (RES) q = unpack8(*ring.slot(stage, 2, k));
+            Eight &gk = g[kWide ? 0 : k], &uk = u[kWide ? 0 : k];
+            if constexpr (kWide) {
+                gk = unpack8(*ring.slot(stage, 0, k));
+                uk = unpack8(*ring.slot(stage, 1, k));
+                const Eight w = gain_of(k);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e = fmaf(-u[k][i], c, g[k][i]);
-                q[i] = RES ? fmaf(r, e, q[i]) : r * e;
+                for (int i = 0; i < 4; ++i) {
+                    uk.p[i] = __fmul2_rn(uk.p[i], splat(r));
+                    gk.p[i] = __fmul2_rn(gk.p[i], w.p[i]);
+                }
             }
-            *reinterpret_cast<uint4 *>(a.dx + row * a.ld_dx + 8 * (t + k * 32 * WPR)) = pack8(q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 e = __ffma2_rn(uk.p[i], splat(c), gk.p[i]);
+                q.p[i] = RES ? __ffma2_rn(splat(r), e, q.p[i]) : __fmul2_rn(splat(r), e);
+            }
+            *reinterpret_cast<uint4 *>(a.dx + row * a.ld_dx + col) = pack8(q);
         }
+        stage = stage == R::kStages - 1 ? 0 : stage + 1;
     }
+    copies_wait<0>();
     if (a.partials) {
-        float *p = a.partials + (int64_t)(first + group) * a.cols;
+        float *p = a.partials + (first + group) * a.cols;
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (in[k]) {
-                float4 *q = reinterpret_cast<float4 *>(p + 8 * (t + k * 32 * WPR));
-                q[0] = make_float4(dgain[k][0], dgain[k][1], dgain[k][2], dgain[k][3]);
-                q[1] = make_float4(dgain[k][4], dgain[k][5], dgain[k][6], dgain[k][7]);
-            }
+        for (int k = 0; k < V; ++k) {
+            const int col = 8 * (t + k * 32 * WPR);
+            if (col >= a.cols) continue;
+            float4 *q = reinterpret_cast<float4 *>(p + col);
+            q[0] = make_float4(dgain[k].p[0].x, dgain[k].p[0].y, dgain[k].p[1].x, dgain[k].p[1].y);
+            q[1] = make_float4(dgain[k].p[2].x, dgain[k].p[2].y, dgain[k].p[3].x, dgain[k].p[3].y);
+        }
     }
 }
 
@@ -481,14 +537,25 @@ Shape shape_for(int64_t cols)
     return {32, 4};
 }
 
-// CTAs of a kernel that an SM holds (asked once: the same on every device of this family).
+// CTAs of a kernel that an SM holds, with its dynamic shared memory allowed for (asked once: the same on every device of this family; the
+// allowance is per device).
 template <auto Kernel>
-int resident(int threads)
+int resident(int threads, int smem)
 {
-    static const int n = [threads] {
-        int k = 0;
-        return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, Kernel, threads, 0) == cudaSuccess && k > 0 ? k : 1;
-    }();
+    static std::atomic<uint64_t> allowed{0};   // a bit per device
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (!(allowed.load(std::memory_order_relaxed) & bit) || dev > 63) {
+        if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return 0;
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
+    static std::atomic<int> known{0};
+    int n = known.load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, Kernel, threads, smem) != cudaSuccess || n < 1) return 0;
+        known.store(n, std::memory_order_relaxed);
+    }
     return n;
 }
 
@@ -547,23 +614,31 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     a.rows = (int32_t)t->rows;
     a.cols = (int32_t)t->cols;
     a.gain_f32 = t->gain_dtype == SNIP_OUT_FP32;
-    a.fmt = t->fmt;
     a.eps = t->eps;
     a.inv_cols = (float)(1.0 / (double)t->cols);
     const Shape s = shape_for(t->cols);
-    auto launch = [&](auto wpr, auto v, auto res) {
-        constexpr auto kernel = rmsnorm_kernel<wpr(), v(), res()>;
-        const int64_t want = ceil_div(t->rows, groups_per_cta(wpr())), cap = (int64_t)resident<kernel>(cta_threads(wpr())) * gemm_sm_count();
-        kernel<<<(unsigned)(want < cap ? want : cap), cta_threads(wpr()), 0, st>>>(a);
+    int n = 0;   // 0: a CUDA call failed
+    auto launch = [&](auto wpr, auto v, auto res, auto fmt) {
+        constexpr auto kernel = rmsnorm_kernel<wpr(), v(), res(), fmt()>;
+        constexpr int smem = Ring<wpr(), v(), res() ? 2 : 1>::kBytes;
+        n = resident<kernel>(cta_threads(wpr()), smem);
+        const int64_t want = ceil_div(t->rows, groups_per_cta(wpr())), cap = (int64_t)n * gemm_sm_count();
+        if (n) kernel<<<(unsigned)(want < cap ? want : cap), cta_threads(wpr()), smem, st>>>(a);
+    };
+    auto with_fmt = [&](auto wpr, auto v, auto res) {
+        if (!a.codes) launch(wpr, v, res, Int<SNIP_FMT_BF16>{});
+        else if (t->fmt == SNIP_FMT_FP8_E4M3) launch(wpr, v, res, Int<SNIP_FMT_FP8_E4M3>{});
+        else launch(wpr, v, res, Int<SNIP_FMT_FP4_E2M1>{});
     };
 #define SNIP_LAUNCH(W, V)                                                                       \
     if (s.wpr == W && s.v == V) {                                                               \
-        if (t->residual) launch(Int<W>{}, Int<V>{}, std::true_type{});                          \
-        else launch(Int<W>{}, Int<V>{}, std::false_type{});                                     \
+        if (t->residual) with_fmt(Int<W>{}, Int<V>{}, std::true_type{});                        \
+        else with_fmt(Int<W>{}, Int<V>{}, std::false_type{});                                   \
     }
     SNIP_NORM_SHAPES(SNIP_LAUNCH)
 #undef SNIP_LAUNCH
     SNIP_CUDA_TRY(cudaGetLastError());
+    if (!n) return SNIP_ERR_CUDA;
     if (!dual) return SNIP_OK;
     NormDualArgs d = {};
     d.h = static_cast<const uint16_t *>(t->residual ? t->h : t->x);
@@ -577,12 +652,22 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     d.rows = a.rows; d.cols = a.cols;
     d.tiles_c = (int32_t)ceil_div(t->cols, kTile);
     d.tiles = d.tiles_c * ceil_div(t->rows, kTile);
-    d.gain_f32 = a.gain_f32; d.fmt = t->fmt; d.fmt_t = t->fmt_t;
-    const int64_t cap = (int64_t)kDualCtas * gemm_sm_count();
-    SNIP_CUDA_TRY(cudaFuncSetAttribute(rmsnorm_dual_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(DualShared)));
-    rmsnorm_dual_kernel<<<(unsigned)(d.tiles < cap ? d.tiles : cap), kDualThreads, sizeof(DualShared), st>>>(d);
+    d.gain_f32 = a.gain_f32;
+    auto launch_dual = [&](auto fmt, auto fmt_t) {
+        constexpr auto kernel = rmsnorm_dual_kernel<fmt(), fmt_t()>;
+        n = resident<kernel>(kDualThreads, (int)sizeof(DualShared));
+        const int64_t cap = (int64_t)n * gemm_sm_count();
+        if (n) kernel<<<(unsigned)(d.tiles < cap ? d.tiles : cap), kDualThreads, sizeof(DualShared), st>>>(d);
+    };
+    auto with_fmt_t = [&](auto fmt) {
+        if (t->fmt_t == SNIP_FMT_FP8_E4M3) launch_dual(fmt, Int<SNIP_FMT_FP8_E4M3>{});
+        else launch_dual(fmt, Int<SNIP_FMT_FP4_E2M1>{});
+    };
+    if (!d.codes) with_fmt_t(Int<SNIP_FMT_BF16>{});
+    else if (t->fmt == SNIP_FMT_FP8_E4M3) with_fmt_t(Int<SNIP_FMT_FP8_E4M3>{});
+    else with_fmt_t(Int<SNIP_FMT_FP4_E2M1>{});
     SNIP_CUDA_TRY(cudaGetLastError());
-    return SNIP_OK;
+    return n ? SNIP_OK : SNIP_ERR_CUDA;
 }
 
 extern "C" int snip_rmsnorm_bwd_workspace(int64_t rows, int64_t cols, size_t *ws_bytes)
@@ -642,8 +727,9 @@ extern "C" int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *t, void *ws, size_t ws
     int64_t ctas = 0;
     auto launch = [&](auto wpr, auto v, auto res) {
         constexpr auto kernel = rmsnorm_bwd_kernel<wpr(), v(), res()>;
-        ctas = bwd_ctas(t->rows, wpr(), resident<kernel>(cta_threads(wpr())));
-        kernel<<<(unsigned)ctas, cta_threads(wpr()), 0, st>>>(a);
+        constexpr int smem = Ring<wpr(), v(), res() ? 3 : 2>::kBytes;
+        ctas = bwd_ctas(t->rows, wpr(), resident<kernel>(cta_threads(wpr()), smem));
+        if (ctas) kernel<<<(unsigned)ctas, cta_threads(wpr()), smem, st>>>(a);
     };
 #define SNIP_LAUNCH(W, V)                                                                       \
     if (s.wpr == W && s.v == V) {                                                               \
@@ -653,6 +739,7 @@ extern "C" int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *t, void *ws, size_t ws
     SNIP_NORM_SHAPES(SNIP_LAUNCH)
 #undef SNIP_LAUNCH
     SNIP_CUDA_TRY(cudaGetLastError());
+    if (!ctas) return SNIP_ERR_CUDA;
     if (t->dgain) {
         dgain_reduce_kernel<<<(unsigned)ceil_div(t->cols, 32), dim3(32, 32), 0, st>>>(a.partials, (int)(ctas * groups_per_cta(s.wpr)), a.cols, t->dgain, t->accumulate);
         SNIP_CUDA_TRY(cudaGetLastError());
