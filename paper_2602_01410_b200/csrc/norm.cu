@@ -24,6 +24,8 @@ int gemm_sm_count();
 namespace {
 
 constexpr int64_t kMaxCols = 32768;
+template <int N>
+using Int = std::integral_constant<int, N>;
 
 struct NormArgs {
     const uint16_t *x, *residual;
@@ -32,9 +34,9 @@ struct NormArgs {
     float *rstd;
     uint8_t *codes;
     float *scales;
-    int64_t ld_x, ld_residual, ld_h, ld_y;
+    int32_t ld_x, ld_residual, ld_h, ld_y;   // 32 bits (checked on the host): index products are 32 x 32 -> 64-bit multiplies
     int32_t rows, cols;
-    int gain_f32;
+    int gain_f32, wpr;
     float eps, inv_cols;
 };
 
@@ -44,9 +46,9 @@ struct NormBwdArgs {
     const float *rstd;
     uint16_t *dx;
     float *partials;   // [groups of the grid][cols], or null
-    int64_t ld_dy, ld_h, ld_dresidual, ld_dx;
+    int32_t ld_dy, ld_h, ld_dresidual, ld_dx;
     int32_t rows, cols;
-    int gain_f32;
+    int gain_f32, wpr;
     float inv_cols;
 };
 
@@ -86,16 +88,16 @@ __device__ __forceinline__ float most8(const Eight &y)
 
 // Codes of eight neighbouring elements under one scale.
 template <int FMT>
-__device__ __forceinline__ void store_codes8(uint8_t *codes, int64_t at, const Eight &y, float s)
+__device__ __forceinline__ void store_codes8(uint8_t *to, const Eight &y, float s)
 {
     float2 t[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) t[i] = __fmul2_rn(y.p[i], splat(s));
     if constexpr (FMT == SNIP_FMT_FP8_E4M3) {
-        *reinterpret_cast<uint2 *>(codes + at) = make_uint2(__byte_perm(cvt_e4m3x2(t[0].x, t[0].y), cvt_e4m3x2(t[1].x, t[1].y), 0x5410),
+        *reinterpret_cast<uint2 *>(to) = make_uint2(__byte_perm(cvt_e4m3x2(t[0].x, t[0].y), cvt_e4m3x2(t[1].x, t[1].y), 0x5410),
                                                             __byte_perm(cvt_e4m3x2(t[2].x, t[2].y), cvt_e4m3x2(t[3].x, t[3].y), 0x5410));
     } else {
-        *reinterpret_cast<uint32_t *>(codes + at / 2) = cvt_e2m1x2(t[0].x, t[0].y) | cvt_e2m1x2(t[1].x, t[1].y) << 8 | cvt_e2m1x2(t[2].x, t[2].y) << 16 |
+        *reinterpret_cast<uint32_t *>(to) = cvt_e2m1x2(t[0].x, t[0].y) | cvt_e2m1x2(t[1].x, t[1].y) << 8 | cvt_e2m1x2(t[2].x, t[2].y) << 16 |
                                                         cvt_e2m1x2(t[3].x, t[3].y) << 24;
     }
 }
@@ -108,132 +110,225 @@ __device__ __forceinline__ Eight load_gain8(const void *gain, int f32, int col)
     return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
 }
 
-// 16 bytes into this thread's own slot of shared memory (read back by itself: nothing to wait for but its own copies), or zeros.
-__device__ __forceinline__ void copy_async(uint4 *slot, const uint16_t *src, bool there)
+// 16 bytes into this thread's own slot of shared memory (read back by itself: nothing to wait for but its own copies).
+__device__ __forceinline__ void copy_async(uint4 *slot, const uint16_t *src)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(slot)), "l"(src), "r"(there ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(slot)), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Sum over the WPR warps of a row group, in a fixed order; the same value in every thread.  `slots` (one float per warp of the CTA) is free again
-// when all threads have come past the next call's barrier: callers alternate between two sets.
-template <int WPR>
-__device__ __forceinline__ float group_sum(float v, float *slots)
+// Where a thread is: `wpr` warps per row, groups of rows side by side in the CTA (warps behind the last group have no row).  Vector k of thread t of
+// a group starts at column col0 + k apart, so that 16 neighbouring threads hold a 128-long tile.
+struct Place {
+    int warp, lane, group, groups, col0, apart;   // warp: of the CTA
+    __device__ __forceinline__ explicit Place(int wpr)
+    {
+        warp = (int)threadIdx.x >> 5;
+        lane = (int)threadIdx.x & 31;
+        groups = (int)(blockDim.x >> 5) / wpr;
+        group = warp / wpr;
+        col0 = 8 * (32 * (warp - group * wpr) + lane);
+        apart = 256 * wpr;
+    }
+};
+
+// Sum over the warps of a row group, in a fixed order; the same value in every thread.  `slots`: 32 floats, zero at first (groups of up to eight
+// warps have eight each), free again when all threads have come past the next call's barrier: callers alternate between two sets.
+__device__ __forceinline__ float group_sum(float v, float *slots, const Place &at, int wpr)
 {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
-    if constexpr (WPR > 1) {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        if (lane == 0) slots[warp] = v;
-        __syncthreads();
-        v = lane < WPR ? slots[warp / WPR * WPR + lane] : 0.0f;
-#pragma unroll
-        for (int off = WPR / 2; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
-        v = __shfl_sync(0xFFFFFFFFu, v, 0);
+    if (wpr == 1) return v;
+    const int first = wpr <= 8 ? 8 * at.group : 0;
+    if (at.lane == 0) slots[wpr <= 8 ? first + at.warp - at.group * wpr : at.warp] = v;
+    __syncthreads();
+    if (wpr <= 8) {
+        const float4 p = *reinterpret_cast<const float4 *>(slots + first), q = *reinterpret_cast<const float4 *>(slots + first + 4);
+        return ((p.x + p.y) + (p.z + p.w)) + ((q.x + q.y) + (q.z + q.w));
     }
+    v = slots[at.lane];
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
     return v;
 }
 
-__host__ __device__ constexpr int cta_threads(int wpr) { return wpr < 8 ? 256 : 32 * wpr; }
-__host__ __device__ constexpr int groups_per_cta(int wpr) { return cta_threads(wpr) / (32 * wpr); }
-
-// Rows on their way: a thread's slots for kStages rows of N arrays of V vectors.
-template <int WPR, int V, int N>
+// Rows on their way: a thread's slots for STAGES rows of N arrays of V vectors (read back by the thread itself).  A vector beyond the last column
+// is never fetched: its slots are zeroed once.
+template <int V, int N, int STAGES>
 struct Ring {
-    static constexpr int kRowBytes = N * V * cta_threads(WPR) * 16;
-    static constexpr int kStages = kRowBytes > 100 * 1024 ? 1 : kRowBytes > 24 * 1024 ? 2 : kRowBytes > 12 * 1024 ? 3 : 4;
-    static constexpr int kBytes = kStages * kRowBytes;
-    static_assert(kBytes <= 224 * 1024, "an SM has 227 KB");
-    uint4 *base;
-    __device__ __forceinline__ uint4 *slot(int stage, int array, int k) const { return base + ((stage * N + array) * V + k) * cta_threads(WPR) + threadIdx.x; }
+    uint4 *mine;
+    __device__ __forceinline__ uint4 *slot(int stage, int array, int k) const { return mine + ((stage * N + array) * V + k) * (int)blockDim.x; }
+    __device__ __forceinline__ Ring(uint8_t *raw, const bool (&in)[V]) : mine(reinterpret_cast<uint4 *>(raw) + threadIdx.x)
+    {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (!in[k])
+                for (int i = 0; i < STAGES * N; ++i) *slot(0, i, k) = make_uint4(0u, 0u, 0u, 0u);
+    }
 };
 
-// WPR warps per row, V vectors of eight elements per thread: vector k of thread t of the group starts at column 8 (t + k 32 WPR), so
-// that 16 neighbouring threads hold a 128-long tile.  FMT: format of the row-tile codes, BF16 for none.
-template <int WPR, int V, bool RES, int FMT>
-__global__ void __launch_bounds__(cta_threads(WPR)) rmsnorm_kernel(const NormArgs a)
+// Scales of the tiles that a thread's V vectors belong to: 16 neighbouring threads hold a tile each.  While the maxima are combined a thread
+// comes to look after one of the vectors only (own_vector), so that there is one division for all of them; the scales are handed round at
+// the end.  Returns the own one.
+template <int V>
+__device__ __forceinline__ int own_vector(int lane) { return (lane & 15) / (16 / V); }
+template <int FMT, int V>
+__device__ __forceinline__ float tile_scales(float (&most)[V], float (&s)[V], int lane)
 {
-    extern __shared__ __align__(16) uint8_t raw[];
-    __shared__ float slots[2][32];
-    using R = Ring<WPR, V, RES ? 2 : 1>;
-    const R ring = {reinterpret_cast<uint4 *>(raw)};
-    constexpr int kGroups = groups_per_cta(WPR);
-    const int t = threadIdx.x % (32 * WPR), group = threadIdx.x / (32 * WPR);
-    const int64_t step = (int64_t)gridDim.x * kGroups;
-    auto fetch = [&](int stage, int64_t row) {
+    if constexpr (V == 4) {
+        const bool upper = (lane & 8) != 0;
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int col = 8 * (t + k * 32 * WPR);
-            const bool there = col < a.cols && row < a.rows;
-            copy_async(ring.slot(stage, 0, k), a.x + (there ? row * a.ld_x + col : 0), there);
-            if (RES) copy_async(ring.slot(stage, 1, k), a.residual + (there ? row * a.ld_residual + col : 0), there);
+        for (int i = 0; i < 2; ++i) {
+            const float give = upper ? most[i] : most[i + 2], keep = upper ? most[i + 2] : most[i];
+            most[i] = fmaxf(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 8));
+        }
+    }
+    if constexpr (V >= 2) {
+        constexpr int kOff = V == 4 ? 4 : 8;
+        const bool upper = (lane & kOff) != 0;
+        const float give = upper ? most[0] : most[1], keep = upper ? most[1] : most[0];
+        most[0] = fmaxf(keep, __shfl_xor_sync(0xFFFFFFFFu, give, kOff));
+    }
+#pragma unroll
+    for (int off = 8 / V; off > 0; off >>= 1) most[0] = fmaxf(most[0], __shfl_xor_sync(0xFFFFFFFFu, most[0], off));
+    const float own = tile_scale<FMT>(most[0], 0);
+#pragma unroll
+    for (int k = 0; k < V; ++k) s[k] = V == 1 ? own : __shfl_sync(0xFFFFFFFFu, own, (lane & 16) | k * (16 / V));
+    return own;
+}
+
+// FMT: format of the row-tile codes, BF16 for none.  THREADS is the CTA's size (so that every slot is at a constant place of the ring, whose turns
+// are written out): warps that no row is dealt to look on.
+template <int V, int THREADS, int STAGES, bool RES, int FMT>
+__global__ void __launch_bounds__(THREADS) rmsnorm_kernel(const NormArgs a)
+{
+    extern __shared__ __align__(128) uint8_t raw[];
+    __shared__ __align__(16) float slots[2][32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the kernel of the transposed copy, which waits for this one
+    const Place at(a.wpr);
+    constexpr int N = RES ? 2 : 1, kPerByte = FMT == SNIP_FMT_FP4_E2M1 ? 2 : 1;
+    uint4 *const mine = reinterpret_cast<uint4 *>(raw) + threadIdx.x;
+    auto slot = [&](int stage, int array, int k) { return mine + ((stage * N + array) * V + k) * THREADS; };
+    const int step = (int)gridDim.x * at.groups, first = (int)blockIdx.x * at.groups, row0 = at.group < at.groups ? first + at.group : a.rows;
+    bool in[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        in[k] = at.group < at.groups && at.col0 + k * at.apart < a.cols;
+        if (!in[k])   // never fetched
+#pragma unroll
+            for (int i = 0; i < STAGES * N; ++i) *slot(0, i, k) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (threadIdx.x < 64) slots[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
+    __syncthreads();
+    // of the widest rows neither the gain nor the row in binary32 stays in registers
+    constexpr bool kWide = V > 2 && THREADS > 512;
+    auto gain_of = [&](int k) { return in[k] ? load_gain8(a.gain, a.gain_f32, at.col0 + k * at.apart) : zeros8(); };
+    // addresses move from row to row; those of rows behind the last are not used
+    const uint16_t *px = a.x + (int64_t)row0 * a.ld_x + at.col0, *pr = RES ? a.residual + (int64_t)row0 * a.ld_residual + at.col0 : nullptr;
+    const int64_t dx = (int64_t)step * a.ld_x, dr = RES ? (int64_t)step * a.ld_residual : 0;
+    int64_t ahead = row0;
+    auto fetch = [&](int stage) {
+        if (ahead < a.rows) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (in[k]) {
+                    copy_async(slot(stage, 0, k), px + k * at.apart);
+                    if (RES) copy_async(slot(stage, 1, k), pr + k * at.apart);
+                }
         }
         copies_commit();
+        ahead += step;
+        px += dx;
+        if (RES) pr += dr;
     };
-    int64_t row = (int64_t)blockIdx.x * kGroups + group;
 #pragma unroll
-    for (int i = 0; i < R::kStages - 1; ++i) fetch(i, row + i * step);
-    // of the widest rows neither the gain nor the row in binary32 stays in registers
-    constexpr bool kWide = V > 2;
+    for (int i = 0; i < STAGES - 1; ++i) fetch(i);
     Eight gain[kWide ? 1 : V];
     if constexpr (!kWide) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int col = 8 * (t + k * 32 * WPR);
-            gain[k] = col < a.cols ? load_gain8(a.gain, a.gain_f32, col) : zeros8();
-        }
+        for (int k = 0; k < V; ++k) gain[k] = gain_of(k);
     }
-    int parity = 0, stage = 0;
-    // all groups of a CTA take the same number of turns: rows behind the last are zeros that nothing is written for
-    for (int64_t base = (int64_t)blockIdx.x * kGroups; base < a.rows; base += step, row += step, parity ^= 1) {
-        fetch(stage == 0 ? R::kStages - 1 : stage - 1, row + (R::kStages - 1) * step);
-        copies_wait<R::kStages - 1>();
+    const int own = own_vector<V>(at.lane), own_col = at.col0 - 8 * (at.lane & 15) + own * at.apart;
+    float *ps = FMT != SNIP_FMT_BF16 && own_col < a.cols && (at.lane & (16 / V - 1)) == 0 ? a.scales + (int64_t)(own_col >> 7) * a.rows + row0 : nullptr;
+    uint8_t *pc = FMT == SNIP_FMT_BF16 ? nullptr : a.codes + ((int64_t)row0 * a.cols + at.col0) / kPerByte;
+    const int64_t dc = (int64_t)step * a.cols / kPerByte;
+    uint16_t *ph = RES ? a.h + (int64_t)row0 * a.ld_h + at.col0 : nullptr;
+    const int64_t dh = RES ? (int64_t)step * a.ld_h : 0;
+    int64_t row = row0;
+    int parity = 0;
+    auto turn = [&](auto which) {
+        constexpr int kStage = decltype(which)::value;
+        fetch(kStage == 0 ? STAGES - 1 : kStage - 1);
+        copies_wait<STAGES - 1>();
+        const bool live = row < a.rows;
         Eight h[kWide ? 1 : V];
         uint4 packed[V];
         float2 sum = splat(0.0f);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const int col = 8 * (t + k * 32 * WPR);
-            packed[k] = *ring.slot(stage, 0, k);
+            packed[k] = *slot(kStage, 0, k);
             Eight e = unpack8(packed[k]);
             if (RES) {
-                const Eight q = unpack8(*ring.slot(stage, 1, k));
+                const Eight q = unpack8(*slot(kStage, 1, k));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) e.p[i] = __fadd2_rn(e.p[i], q.p[i]);
                 packed[k] = pack8(e);
-                if (col < a.cols && row < a.rows) *reinterpret_cast<uint4 *>(a.h + row * a.ld_h + col) = packed[k];
+                if (live && in[k]) *reinterpret_cast<uint4 *>(ph + k * at.apart) = packed[k];
                 e = unpack8(packed[k]);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum = __ffma2_rn(e.p[i], e.p[i], sum);
             if constexpr (!kWide) h[k] = e;
         }
-        stage = stage == R::kStages - 1 ? 0 : stage + 1;
-        const float total = group_sum<WPR>(sum.x + sum.y, slots[parity]);
-        const float rstd = __frcp_rn(__fsqrt_rn(fmaf(total, a.inv_cols, a.eps)));
-        if (t == 0 && a.rstd && row < a.rows) a.rstd[row] = rstd;
-        if (FMT == SNIP_FMT_BF16 && !a.y) continue;
+        const float total = group_sum(sum.x + sum.y, slots[parity], at, a.wpr);
+        const float rstd = rsqrtf(fmaf(total, a.inv_cols, a.eps));
+        if (at.col0 == 0 && a.rstd && live) a.rstd[row] = rstd;
+        if (FMT != SNIP_FMT_BF16 || a.y) {
+            Eight y[V];
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int col = 8 * (t + k * 32 * WPR);
-            const bool ok = col < a.cols && row < a.rows;
-            Eight y;
-            if constexpr (kWide) y = scaled8(unpack8(packed[k]), rstd, col < a.cols ? load_gain8(a.gain, a.gain_f32, col) : zeros8());
-            else y = scaled8(h[k], rstd, gain[k]);
-            if (a.y && ok) *reinterpret_cast<uint4 *>(a.y + row * a.ld_y + col) = pack8(y);
+            for (int k = 0; k < V; ++k) {
+                if constexpr (kWide) y[k] = scaled8(unpack8(packed[k]), rstd, gain_of(k));
+                else y[k] = scaled8(h[k], rstd, gain[k]);
+            }
+            if (a.y && live) {
+                uint16_t *py = a.y + row * a.ld_y + at.col0;
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (in[k]) *reinterpret_cast<uint4 *>(py + k * at.apart) = pack8(y[k]);
+            }
             if constexpr (FMT != SNIP_FMT_BF16) {
-                float most = most8(y);
+                float most[V], s[V];
 #pragma unroll
-                for (int off = 8; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, off));
-                const float s = tile_scale<FMT>(most, 0);
-                if (ok) {
-                    if ((t & 15) == 0) a.scales[(int64_t)(col >> 7) * a.rows + row] = s;
-                    store_codes8<FMT>(a.codes, row * a.cols + col, y, s);
+                for (int k = 0; k < V; ++k) most[k] = most8(y[k]);
+                const float one = tile_scales<FMT, V>(most, s, at.lane);
+                if (live) {
+                    if (ps) *ps = one;
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        if (in[k]) store_codes8<FMT>(pc + k * at.apart / kPerByte, y[k], s[k]);
                 }
+                if (ps) ps += step;
+                pc += dc;
             }
         }
+        row += step;
+        if (RES) ph += dh;
+        parity ^= 1;
+    };
+    // all groups of a CTA take the same number of turns: nothing is written for rows behind the last
+    for (int64_t base = first; base < a.rows;) {
+        turn(Int<0>{});
+        if constexpr (STAGES > 1) {
+            if ((base += step) >= a.rows) break;
+            turn(Int<1>{});
+        }
+        if constexpr (STAGES > 2) {
+            if ((base += step) >= a.rows) break;
+            turn(Int<2>{});
+        }
+        base += step;
     }
     copies_wait<0>();
 }
@@ -247,9 +342,7 @@ struct NormDualArgs {
     const float *rstd;
     uint8_t *codes, *codes_t;
     float *scales, *scales_t;
-    int64_t ld;
-    int32_t rows, cols, tiles_c;
-    int64_t tiles;
+    int32_t rows, cols, tiles_c, tiles, ld;
     int gain_f32;
 };
 constexpr int kTile = 128;
@@ -271,17 +364,27 @@ __global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(c
     extern __shared__ __align__(128) uint8_t raw[];
     DualShared &m = *reinterpret_cast<DualShared *>(raw);
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31, warp = tid >> 5;
-    auto fetch = [&](int64_t tile) {
-        const int64_t row = tile / a.tiles_c * kTile + 8 * ty, col = tile % a.tiles_c * kTile + 8 * tx;
-        const bool ok = tile < a.tiles && row < a.rows && col < a.cols;
-        const uint16_t *p = a.h + (ok ? row * a.ld + col : 0);
+    // row and column of the tile, moved on without a division
+    const int step_r = (int)gridDim.x / a.tiles_c, step_c = (int)gridDim.x % a.tiles_c;
+    auto advance = [&](int &r, int &c) {
+        r += step_r;
+        c += step_c;
+        if (c >= a.tiles_c) { c -= a.tiles_c; ++r; }
+    };
+    auto fetch = [&](int tile, int r, int c) {
+        if (tile < a.tiles && r * kTile + 8 * ty < a.rows && c * kTile + 8 * tx < a.cols) {
+            const uint16_t *p = a.h + (int64_t)(r * kTile + 8 * ty) * a.ld + c * kTile + 8 * tx;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) copy_async(&m.slot[i][tid], p + (ok ? i * a.ld : 0), ok);
+            for (int i = 0; i < 8; ++i) copy_async(&m.slot[i][tid], p + (int64_t)i * a.ld);
+        }
         copies_commit();
     };
-    fetch(blockIdx.x);
-    for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const int tr = (int)(tile / a.tiles_c), tc = (int)(tile % a.tiles_c);
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // for the kernel that leaves h and rstd
+    int tr = (int)blockIdx.x / a.tiles_c, tc = (int)blockIdx.x % a.tiles_c;
+    fetch((int)blockIdx.x, tr, tc);
+    for (int tile = (int)blockIdx.x; tile < a.tiles; tile += (int)gridDim.x) {
+        int next_r = tr, next_c = tc;
+        advance(next_r, next_c);
         const int row0 = tr * kTile + 8 * ty, col0 = tc * kTile + 8 * tx;
         const bool ok = row0 < a.rows && col0 < a.cols;
         Eight gain = zeros8();
@@ -296,7 +399,8 @@ __global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(c
         copies_wait<0>();
         float rmax[8], cmax[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) cmax[i] = 0.0f;
+        for (int i = 0; i < 8; ++i) rmax[i] = cmax[i] = 0.0f;
+        if (ok) {   // (the slots of what a ragged tile lacks hold anything)
 #pragma unroll
         for (int p = 0; p < 8; p += 2) {
             const Eight y0 = scaled8(unpack8(m.slot[p][tid]), rstd[p], gain), y1 = scaled8(unpack8(m.slot[p + 1][tid]), rstd[p + 1], gain);
@@ -307,6 +411,7 @@ __global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(c
                 cmax[2 * i] = fmaxf(fmaxf(cmax[2 * i], fabsf(y0.p[i].x)), fabsf(y1.p[i].x));
                 cmax[2 * i + 1] = fmaxf(fmaxf(cmax[2 * i + 1], fabsf(y0.p[i].y)), fabsf(y1.p[i].y));
             }
+        }
         }
         if constexpr (FMT != SNIP_FMT_BF16) {
             // rows: each step halves the number of rows a lane still looks after; lanes 2 q and 2 q + 1 of a half-warp end with row q's maximum
@@ -350,6 +455,8 @@ __global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(c
             const float4 p = *reinterpret_cast<const float4 *>(&m.col_scale[8 * tx]), q = *reinterpret_cast<const float4 *>(&m.col_scale[8 * tx + 4]);
             cs = {{make_float2(p.x, p.y), make_float2(p.z, p.w), make_float2(q.x, q.y), make_float2(q.z, q.w)}};
         }
+        const int line = FMT == SNIP_FMT_FP4_E2M1 ? a.cols >> 1 : a.cols;
+        uint8_t *pc = FMT == SNIP_FMT_BF16 ? nullptr : a.codes + (int64_t)row0 * line + (FMT == SNIP_FMT_FP4_E2M1 ? col0 >> 1 : col0);
         uint32_t ct[8][2];   // column i: codes of its eight rows (FP4: the first word)
 #pragma unroll
         for (int p = 0; p < 8; p += 4) {
@@ -362,7 +469,7 @@ __global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(c
                     const int r = p + e + f;
                     y[f] = scaled8(unpack8(m.slot[r][tid]), rstd[r], gain);
                     if constexpr (FMT != SNIP_FMT_BF16)
-                        if (ok) store_codes8<FMT>(a.codes, (int64_t)(row0 + r) * a.cols + col0, y[f], m.row_scale[8 * ty + r]);
+                        if (ok) store_codes8<FMT>(pc + (int64_t)r * line, y[f], m.row_scale[8 * ty + r]);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -382,124 +489,143 @@ __global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(c
                 else ct[i][p >> 2] = __byte_perm(part[0][i], part[1][i], 0x0040);   // two bytes
             }
         }
-        fetch(tile + gridDim.x);   // the slot has been read
+        fetch(tile + (int)gridDim.x, next_r, next_c);   // the slot has been read
         // transposed codes: line = column of the tile, 128 (64) bytes each; 16-byte pieces swizzled by the line so that neither side conflicts
         constexpr bool kFp8T = FMT_T == SNIP_FMT_FP8_E4M3;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int line = 8 * tx + i;
-            if constexpr (kFp8T) *reinterpret_cast<uint2 *>(&m.stage[line * 128 + ((ty >> 1) ^ (tx & 7)) * 16 + (ty & 1) * 8]) = make_uint2(ct[i][0], ct[i][1]);
-            else *reinterpret_cast<uint32_t *>(&m.stage[line * 64 + ((ty >> 2) ^ (tx & 3)) * 16 + (ty & 3) * 4]) = __byte_perm(ct[i][0], ct[i][1], 0x5410);
+            const int to = 8 * tx + i;
+            if constexpr (kFp8T) *reinterpret_cast<uint2 *>(&m.stage[to * 128 + ((ty >> 1) ^ (tx & 7)) * 16 + (ty & 1) * 8]) = make_uint2(ct[i][0], ct[i][1]);
+            else *reinterpret_cast<uint32_t *>(&m.stage[to * 64 + ((ty >> 2) ^ (tx & 3)) * 16 + (ty & 3) * 4]) = __byte_perm(ct[i][0], ct[i][1], 0x5410);
         }
         __syncthreads();
         constexpr int kPieces = kFp8T ? 8 : 4, kRows = kFp8T ? 16 : 32;   // 16-byte pieces of a line, rows in one
 #pragma unroll
         for (int j = 0; j < kTile * kPieces / kDualThreads; ++j) {
-            const int line = (j * kDualThreads + tid) / kPieces, piece = tid % kPieces;
-            const int row = tr * kTile + piece * kRows, col = tc * kTile + line;
+            const int from = (j * kDualThreads + tid) / kPieces, piece = tid % kPieces;
+            const int row = tr * kTile + piece * kRows, col = tc * kTile + from;
             if (col >= a.cols || row >= a.rows) continue;
             const int64_t elem = (int64_t)col * a.rows + row;
             *reinterpret_cast<uint4 *>(a.codes_t + (kFp8T ? elem : elem / 2)) =
-                *reinterpret_cast<const uint4 *>(&m.stage[line * (16 * kPieces) + (piece ^ ((line >> 3) & (kPieces - 1))) * 16]);
+                *reinterpret_cast<const uint4 *>(&m.stage[from * (16 * kPieces) + (piece ^ ((from >> 3) & (kPieces - 1))) * 16]);
         }
+        tr = next_r;
+        tc = next_c;
     }
     copies_wait<0>();
 }
 
-template <int WPR, int V, bool RES>
-__global__ void __launch_bounds__(cta_threads(WPR)) rmsnorm_bwd_kernel(const NormBwdArgs a)
+template <int V, int THREADS, int STAGES, bool RES>
+__global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(const NormBwdArgs a)
 {
-    extern __shared__ __align__(16) uint8_t raw[];
-    __shared__ float slots[2][32];
-    using R = Ring<WPR, V, RES ? 3 : 2>;
-    const R ring = {reinterpret_cast<uint4 *>(raw)};
-    constexpr int kGroups = groups_per_cta(WPR);
-    const int t = threadIdx.x % (32 * WPR), group = threadIdx.x / (32 * WPR);
-    const int64_t step = (int64_t)gridDim.x * kGroups, first = (int64_t)blockIdx.x * kGroups;
-    auto fetch = [&](int stage, int64_t row) {
+    extern __shared__ __align__(128) uint8_t raw[];
+    __shared__ __align__(16) float slots[2][32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the reduction of the gain's gradient, which waits for this kernel
+    const Place at(a.wpr);
+    bool in[V];
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int col = 8 * (t + k * 32 * WPR);
-            const bool there = col < a.cols && row < a.rows;
-            copy_async(ring.slot(stage, 0, k), a.dy + (there ? row * a.ld_dy + col : 0), there);
-            copy_async(ring.slot(stage, 1, k), a.h + (there ? row * a.ld_h + col : 0), there);
-            if (RES) copy_async(ring.slot(stage, 2, k), a.dresidual + (there ? row * a.ld_dresidual + col : 0), there);
+    for (int k = 0; k < V; ++k) in[k] = at.col0 + k * at.apart < a.cols;
+    const Ring<V, RES ? 3 : 2, STAGES> ring(raw, in);
+    if (threadIdx.x < 64) slots[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
+    __syncthreads();
+    const int step = (int)gridDim.x * at.groups, first = (int)blockIdx.x * at.groups, row0 = first + at.group;
+    const uint16_t *py = a.dy + (int64_t)row0 * a.ld_dy + at.col0, *ph = a.h + (int64_t)row0 * a.ld_h + at.col0;
+    const uint16_t *pd = RES ? a.dresidual + (int64_t)row0 * a.ld_dresidual + at.col0 : nullptr;
+    const int64_t sy = (int64_t)step * a.ld_dy, sh = (int64_t)step * a.ld_h, sd = RES ? (int64_t)step * a.ld_dresidual : 0;
+    int64_t ahead = row0;
+    auto fetch = [&](int stage) {
+        if (ahead < a.rows) {
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (in[k]) {
+                    copy_async(ring.slot(stage, 0, k), py + k * at.apart);
+                    copy_async(ring.slot(stage, 1, k), ph + k * at.apart);
+                    if (RES) copy_async(ring.slot(stage, 2, k), pd + k * at.apart);
+                }
         }
         copies_commit();
+        ahead += step;
+        py += sy;
+        ph += sh;
+        if (RES) pd += sd;
     };
-    int64_t row = first + group;
 #pragma unroll
-    for (int i = 0; i < R::kStages - 1; ++i) fetch(i, row + i * step);
+    for (int i = 0; i < STAGES - 1; ++i) fetch(i);
     // of the widest rows neither the gain nor the products stay in registers
     constexpr bool kWide = V > 2;
-    auto gain_of = [&](int k) {
-        const int col = 8 * (t + k * 32 * WPR);
-        return col < a.cols ? load_gain8(a.gain, a.gain_f32, col) : zeros8();
-    };
+    auto gain_of = [&](int k) { return in[k] ? load_gain8(a.gain, a.gain_f32, at.col0 + k * at.apart) : zeros8(); };
     Eight gain[kWide ? 1 : V], dgain[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         if constexpr (!kWide) gain[k] = gain_of(k);
         dgain[k] = zeros8();
     }
+    int64_t row = row0;
     float rstd = row < a.rows ? __ldg(a.rstd + row) : 0.0f;
+    uint16_t *px = a.dx + (int64_t)row0 * a.ld_dx + at.col0;
+    const int64_t sx = (int64_t)step * a.ld_dx;
     int parity = 0, stage = 0;
-    for (int64_t base = first; base < a.rows; base += step, row += step, parity ^= 1) {
-        fetch(stage == 0 ? R::kStages - 1 : stage - 1, row + (R::kStages - 1) * step);
-        copies_wait<R::kStages - 1>();
+    for (int64_t base = first; base < a.rows; base += step, parity ^= 1) {
+        fetch(stage == 0 ? STAGES - 1 : stage - 1);
+        copies_wait<STAGES - 1>();
+        const bool live = row < a.rows;
         Eight g[kWide ? 1 : V], u[kWide ? 1 : V];   // dy gain, h rstd
         float2 dot = splat(0.0f);
         const float r = rstd;
+        if (live) {   // (a group behind the last row: nothing has been fetched, nothing may be added)
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            Eight &gk = g[kWide ? 0 : k], &uk = u[kWide ? 0 : k];
-            gk = unpack8(*ring.slot(stage, 0, k));
-            uk = unpack8(*ring.slot(stage, 1, k));
-            const Eight w = kWide ? gain_of(k) : gain[kWide ? 0 : k];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uk.p[i] = __fmul2_rn(uk.p[i], splat(r));
-                dgain[k].p[i] = __ffma2_rn(gk.p[i], uk.p[i], dgain[k].p[i]);
-                gk.p[i] = __fmul2_rn(gk.p[i], w.p[i]);
-                dot = __ffma2_rn(gk.p[i], uk.p[i], dot);
-            }
-        }
-        if (row + step < a.rows) rstd = __ldg(a.rstd + row + step);
-        const float c = group_sum<WPR>(dot.x + dot.y, slots[parity]) * -a.inv_cols;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int col = 8 * (t + k * 32 * WPR);
-            if (col >= a.cols || row >= a.rows) continue;
-            Eight q;
-            if (RES) q = unpack8(*ring.slot(stage, 2, k));
-            Eight &gk = g[kWide ? 0 : k], &uk = u[kWide ? 0 : k];
-            if constexpr (kWide) {
+            for (int k = 0; k < V; ++k) {
+                Eight &gk = g[kWide ? 0 : k], &uk = u[kWide ? 0 : k];
                 gk = unpack8(*ring.slot(stage, 0, k));
                 uk = unpack8(*ring.slot(stage, 1, k));
-                const Eight w = gain_of(k);
+                const Eight w = kWide ? gain_of(k) : gain[kWide ? 0 : k];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     uk.p[i] = __fmul2_rn(uk.p[i], splat(r));
+                    dgain[k].p[i] = __ffma2_rn(gk.p[i], uk.p[i], dgain[k].p[i]);
                     gk.p[i] = __fmul2_rn(gk.p[i], w.p[i]);
+                    dot = __ffma2_rn(gk.p[i], uk.p[i], dot);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 e = __ffma2_rn(uk.p[i], splat(c), gk.p[i]);
-                q.p[i] = RES ? __ffma2_rn(splat(r), e, q.p[i]) : __fmul2_rn(splat(r), e);
-            }
-            *reinterpret_cast<uint4 *>(a.dx + row * a.ld_dx + col) = pack8(q);
         }
-        stage = stage == R::kStages - 1 ? 0 : stage + 1;
+        row += step;
+        if (row < a.rows) rstd = __ldg(a.rstd + row);
+        const float c = group_sum(dot.x + dot.y, slots[parity], at, a.wpr) * -a.inv_cols;
+        if (live) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                if (!in[k]) continue;
+                Eight q;
+                if (RES) q = unpack8(*ring.slot(stage, 2, k));
+                Eight &gk = g[kWide ? 0 : k], &uk = u[kWide ? 0 : k];
+                if constexpr (kWide) {
+                    gk = unpack8(*ring.slot(stage, 0, k));
+                    uk = unpack8(*ring.slot(stage, 1, k));
+                    const Eight w = gain_of(k);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uk.p[i] = __fmul2_rn(uk.p[i], splat(r));
+                        gk.p[i] = __fmul2_rn(gk.p[i], w.p[i]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 e = __ffma2_rn(uk.p[i], splat(c), gk.p[i]);
+                    q.p[i] = RES ? __ffma2_rn(splat(r), e, q.p[i]) : __fmul2_rn(splat(r), e);
+                }
+                *reinterpret_cast<uint4 *>(px + k * at.apart) = pack8(q);
+            }
+        }
+        px += sx;
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
     copies_wait<0>();
     if (a.partials) {
-        float *p = a.partials + (first + group) * a.cols;
+        float *p = a.partials + (int64_t)row0 * a.cols + at.col0;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const int col = 8 * (t + k * 32 * WPR);
-            if (col >= a.cols) continue;
-            float4 *q = reinterpret_cast<float4 *>(p + col);
+            if (!in[k]) continue;
+            float4 *q = reinterpret_cast<float4 *>(p + k * at.apart);
             q[0] = make_float4(dgain[k].p[0].x, dgain[k].p[0].y, dgain[k].p[1].x, dgain[k].p[1].y);
             q[1] = make_float4(dgain[k].p[2].x, dgain[k].p[2].y, dgain[k].p[3].x, dgain[k].p[3].y);
         }
@@ -510,6 +636,7 @@ __global__ void __launch_bounds__(cta_threads(WPR)) rmsnorm_bwd_kernel(const Nor
 __global__ void __launch_bounds__(1024) dgain_reduce_kernel(const float *partials, int n, int cols, float *dgain, int accumulate)
 {
     __shared__ float part[32][33];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int c = blockIdx.x * 32 + threadIdx.x;
     float v = 0.0f;
     if (c < cols)
@@ -524,56 +651,97 @@ __global__ void __launch_bounds__(1024) dgain_reduce_kernel(const float *partial
     }
 }
 
-// Warps per row and vectors per thread for a row of `cols` elements.
+// How rows of `cols` elements are dealt to threads: vectors per thread, warps per row, rows side by side, stages of the ring.
 struct Shape {
-    int wpr, v;
+    int v, wpr, groups, stages, smem, threads, form;
 };
-Shape shape_for(int64_t cols)
+// Forward: CTAs of fixed sizes, as F(form, V, threads, stages).
+#define SNIP_NORM_FWD_FORMS(F) F(0, 1, 256, 3) F(1, 1, 512, 3) F(2, 1, 1024, 3) F(3, 2, 256, 3) F(4, 2, 512, 3) F(5, 4, 512, 2) F(6, 4, 1024, 1) F(7, 4, 256, 2)
+// More vectors per thread spread what a row costs over more elements; fewer leave more threads to fetch.  16384 x 4096 with two / four vectors in us:
+// residual added 65.3 / 63.4, and y written 91.8 / 89.4, and FP8 codes 83.0 / 83.1 (8192 x 8192: 79.7 / 83.1); no residual: rstd alone 21.5 / 23.8,
+// y 47.5 / 43.7, codes 41.6 / 37.9.  2048 columns: 21.3 / 22.2.
+Shape fwd_shape(int64_t cols, bool residual, bool y, bool codes, bool few)
 {
-    const int64_t vecs = ceil_div(cols, 8 * 32);   // vectors per lane of one warp
-    for (int wpr : {1, 4, 8, 16, 32})
-        for (int v : {1, 2})
-            if (vecs <= (int64_t)wpr * v) return {wpr, v};
-    return {32, 4};
+    Shape s;
+    const bool four = cols > 2048 && (residual ? !codes : codes || y);
+    s.v = cols > 8192 ? 4 : few ? 1 : four ? 4 : 2;
+    s.wpr = (int)ceil_div(cols, 256 * s.v);
+    s.threads = s.wpr <= 8 ? 256 : s.wpr <= 16 ? 512 : 1024;
+    s.groups = s.threads / 32 / s.wpr;
+    s.form = s.v == 1 ? (s.threads == 256 ? 0 : s.threads == 512 ? 1 : 2) : s.v == 2 ? (s.threads == 256 ? 3 : 4) : s.threads == 512 ? 5 : s.threads == 1024 ? 6 : 7;
+    s.stages = s.form < 5 ? 3 : s.form == 6 ? 1 : 2;
+    s.smem = s.stages * (residual ? 2 : 1) * s.v * s.threads * 16;   // at most 128 KB
+    return s;
 }
+// Backward: as F(form, V, most threads, stages).
+#define SNIP_NORM_BWD_FORMS(F) F(0, 1, 1024, 3) F(1, 2, 512, 3) F(2, 2, 512, 2) F(3, 4, 512, 2) F(4, 4, 1024, 1)
+Shape bwd_shape(int64_t cols, int arrays, bool few)
+{
+    Shape s;
+    s.v = cols > 8192 ? 4 : few ? 1 : 2;
+    s.wpr = (int)ceil_div(cols, 256 * s.v);
+    s.groups = s.wpr >= 8 ? 1 : 8 / s.wpr;
+    s.threads = 32 * s.wpr * s.groups;
+    const int row_bytes = arrays * s.v * s.threads * 16;
+    s.form = s.v == 4 ? (s.threads > 512 ? 4 : 3) : s.v == 1 ? 0 : row_bytes <= 32 * 1024 ? 1 : 2;
+    s.stages = s.form == 4 ? 1 : s.form < 2 ? 3 : 2;
+    s.smem = s.stages * row_bytes;   // at most 192 KB
+    return s;
+}
+constexpr int64_t kFewRows = 296;
 
 // CTAs of a kernel that an SM holds, with its dynamic shared memory allowed for (asked once: the same on every device of this family; the
 // allowance is per device).
 template <auto Kernel>
-int resident(int threads, int smem)
+int resident(int threads, int smem, int most_smem)
 {
     static std::atomic<uint64_t> allowed{0};   // a bit per device
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
     const uint64_t bit = 1ull << (dev & 63);
     if (!(allowed.load(std::memory_order_relaxed) & bit) || dev > 63) {
-        if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return 0;
+        if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem) != cudaSuccess) return 0;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
-    static std::atomic<int> known{0};
-    int n = known.load(std::memory_order_relaxed);
+    // by threads: the shared memory goes with them
+    static std::atomic<int> known[33];
+    int n = known[threads / 32].load(std::memory_order_relaxed);
     if (n == 0) {
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, Kernel, threads, smem) != cudaSuccess || n < 1) return 0;
-        known.store(n, std::memory_order_relaxed);
+        known[threads / 32].store(n, std::memory_order_relaxed);
     }
     return n;
 }
 
-// F(WPR, V) of every shape
-#define SNIP_NORM_SHAPES(F) F(1, 1) F(1, 2) F(4, 1) F(4, 2) F(8, 1) F(8, 2) F(16, 1) F(16, 2) F(32, 1) F(32, 2) F(32, 4)
-
-bool bad_ld(int64_t ld, int64_t cols) { return ld < cols || (ld % 8) != 0; }
+bool bad_ld(int64_t ld, int64_t cols) { return ld < cols || (ld % 8) != 0 || ld > INT32_MAX; }
 bool bad_dims(int64_t rows, int64_t cols) { return rows < 0 || rows > INT32_MAX - 128 || cols <= 0 || (cols % 8) != 0 || cols > kMaxCols; }
 
-template <int N>
-using Int = std::integral_constant<int, N>;
+
+constexpr int kMostSmem = 200 * 1024;
 
 // CTAs of the backward pass (each group of rows leaves one partial of dgain).  kBwdCtas bounds the workspace.
 constexpr int64_t kBwdCtas = 8 * 148;
-int64_t bwd_ctas(int64_t rows, int wpr, int per_sm)
+int64_t bwd_ctas(int64_t rows, int groups, int per_sm)
 {
-    const int64_t want = ceil_div(rows, groups_per_cta(wpr)), fit = (int64_t)per_sm * gemm_sm_count(), cap = fit < kBwdCtas ? fit : kBwdCtas;
+    const int64_t want = ceil_div(rows, groups), fit = (int64_t)per_sm * gemm_sm_count(), cap = fit < kBwdCtas ? fit : kBwdCtas;
     return want < cap ? want : cap;
+}
+
+// A kernel that may be set up while the one before it on the stream ends; it waits for that one's results itself.
+template <typename Kernel, typename... Args>
+cudaError_t launch_behind(Kernel kernel, dim3 grid, dim3 block, int smem, cudaStream_t st, const Args &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 }  // namespace
@@ -593,6 +761,7 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     if (t->codes && t->fmt != SNIP_FMT_FP8_E4M3 && t->fmt != SNIP_FMT_FP4_E2M1) return SNIP_ERR_ARG;
     if (t->codes_t && ((t->fmt_t != SNIP_FMT_FP8_E4M3 && t->fmt_t != SNIP_FMT_FP4_E2M1) || !t->rstd)) return SNIP_ERR_ARG;
     if (t->codes_t && ((t->rows % 64) != 0 || (t->cols % 64) != 0)) return SNIP_ERR_SHAPE;
+    if (t->codes_t && ceil_div(t->rows, kTile) * ceil_div(t->cols, kTile) > INT32_MAX / 2) return SNIP_ERR_SHAPE;   // tiles are counted in 32 bits
     if (bad_ld(t->ld_x, t->cols) || (t->residual && (bad_ld(t->ld_residual, t->cols) || bad_ld(t->ld_h, t->cols))) || (t->y && bad_ld(t->ld_y, t->cols))) return SNIP_ERR_SHAPE;
     const void *all[] = {t->x, t->residual, t->gain, t->h, t->y, t->rstd, t->codes, t->scales, t->codes_t, t->scales_t};
     for (const void *p : all)
@@ -610,32 +779,32 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     a.rstd = t->rstd;
     a.codes = dual ? nullptr : static_cast<uint8_t *>(t->codes);
     a.scales = t->scales;
-    a.ld_x = t->ld_x; a.ld_residual = t->ld_residual; a.ld_h = t->ld_h; a.ld_y = t->ld_y;
+    a.ld_x = (int32_t)t->ld_x; a.ld_residual = (int32_t)t->ld_residual; a.ld_h = (int32_t)t->ld_h; a.ld_y = (int32_t)t->ld_y;
     a.rows = (int32_t)t->rows;
     a.cols = (int32_t)t->cols;
     a.gain_f32 = t->gain_dtype == SNIP_OUT_FP32;
     a.eps = t->eps;
     a.inv_cols = (float)(1.0 / (double)t->cols);
-    const Shape s = shape_for(t->cols);
+    const Shape s = fwd_shape(t->cols, t->residual != nullptr, t->y != nullptr, a.codes != nullptr, t->rows <= kFewRows);
+    a.wpr = s.wpr;
     int n = 0;   // 0: a CUDA call failed
-    auto launch = [&](auto wpr, auto v, auto res, auto fmt) {
-        constexpr auto kernel = rmsnorm_kernel<wpr(), v(), res(), fmt()>;
-        constexpr int smem = Ring<wpr(), v(), res() ? 2 : 1>::kBytes;
-        n = resident<kernel>(cta_threads(wpr()), smem);
-        const int64_t want = ceil_div(t->rows, groups_per_cta(wpr())), cap = (int64_t)n * gemm_sm_count();
-        if (n) kernel<<<(unsigned)(want < cap ? want : cap), cta_threads(wpr()), smem, st>>>(a);
+    auto launch = [&](auto v, auto threads, auto stages, auto res, auto fmt) {
+        constexpr auto kernel = rmsnorm_kernel<v(), threads(), stages(), res(), fmt()>;
+        n = resident<kernel>(s.threads, s.smem, kMostSmem);
+        const int64_t want = ceil_div(t->rows, s.groups), cap = (int64_t)n * gemm_sm_count();
+        if (n) kernel<<<(unsigned)(want < cap ? want : cap), s.threads, s.smem, st>>>(a);
     };
-    auto with_fmt = [&](auto wpr, auto v, auto res) {
-        if (!a.codes) launch(wpr, v, res, Int<SNIP_FMT_BF16>{});
-        else if (t->fmt == SNIP_FMT_FP8_E4M3) launch(wpr, v, res, Int<SNIP_FMT_FP8_E4M3>{});
-        else launch(wpr, v, res, Int<SNIP_FMT_FP4_E2M1>{});
+    auto with_fmt = [&](auto v, auto threads, auto stages, auto res) {
+        if (!a.codes) launch(v, threads, stages, res, Int<SNIP_FMT_BF16>{});
+        else if (t->fmt == SNIP_FMT_FP8_E4M3) launch(v, threads, stages, res, Int<SNIP_FMT_FP8_E4M3>{});
+        else launch(v, threads, stages, res, Int<SNIP_FMT_FP4_E2M1>{});
     };
-#define SNIP_LAUNCH(W, V)                                                                       \
-    if (s.wpr == W && s.v == V) {                                                               \
-        if (t->residual) with_fmt(Int<W>{}, Int<V>{}, std::true_type{});                        \
-        else with_fmt(Int<W>{}, Int<V>{}, std::false_type{});                                   \
+#define SNIP_LAUNCH(FORM, V, THREADS, STAGES)                                                   \
+    if (s.form == FORM) {                                                                       \
+        if (t->residual) with_fmt(Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::true_type{});   \
+        else with_fmt(Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::false_type{});              \
     }
-    SNIP_NORM_SHAPES(SNIP_LAUNCH)
+    SNIP_NORM_FWD_FORMS(SNIP_LAUNCH)
 #undef SNIP_LAUNCH
     SNIP_CUDA_TRY(cudaGetLastError());
     if (!n) return SNIP_ERR_CUDA;
@@ -648,16 +817,18 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     d.scales = t->scales;
     d.codes_t = static_cast<uint8_t *>(t->codes_t);
     d.scales_t = t->scales_t;
-    d.ld = t->residual ? t->ld_h : t->ld_x;
+    d.ld = (int32_t)(t->residual ? t->ld_h : t->ld_x);
     d.rows = a.rows; d.cols = a.cols;
     d.tiles_c = (int32_t)ceil_div(t->cols, kTile);
-    d.tiles = d.tiles_c * ceil_div(t->rows, kTile);
+    d.tiles = (int32_t)(d.tiles_c * ceil_div(t->rows, kTile));
     d.gain_f32 = a.gain_f32;
+    cudaError_t e = cudaSuccess;
     auto launch_dual = [&](auto fmt, auto fmt_t) {
         constexpr auto kernel = rmsnorm_dual_kernel<fmt(), fmt_t()>;
-        n = resident<kernel>(kDualThreads, (int)sizeof(DualShared));
+        constexpr int smem = (int)sizeof(DualShared);
+        n = resident<kernel>(kDualThreads, smem, smem);
         const int64_t cap = (int64_t)n * gemm_sm_count();
-        if (n) kernel<<<(unsigned)(d.tiles < cap ? d.tiles : cap), kDualThreads, sizeof(DualShared), st>>>(d);
+        if (n) e = launch_behind(kernel, dim3((unsigned)(d.tiles < cap ? d.tiles : cap)), dim3(kDualThreads), smem, st, d);
     };
     auto with_fmt_t = [&](auto fmt) {
         if (t->fmt_t == SNIP_FMT_FP8_E4M3) launch_dual(fmt, Int<SNIP_FMT_FP8_E4M3>{});
@@ -666,7 +837,7 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     if (!d.codes) with_fmt_t(Int<SNIP_FMT_BF16>{});
     else if (t->fmt == SNIP_FMT_FP8_E4M3) with_fmt_t(Int<SNIP_FMT_FP8_E4M3>{});
     else with_fmt_t(Int<SNIP_FMT_FP4_E2M1>{});
-    SNIP_CUDA_TRY(cudaGetLastError());
+    SNIP_CUDA_TRY(e);
     return n ? SNIP_OK : SNIP_ERR_CUDA;
 }
 
@@ -676,9 +847,9 @@ extern "C" int snip_rmsnorm_bwd_workspace(int64_t rows, int64_t cols, size_t *ws
     if (!ws_bytes) return SNIP_ERR_ARG;
     if (bad_dims(rows, cols)) return SNIP_ERR_SHAPE;
     // one partial per group of rows in flight, of the largest grid
-    const Shape s = shape_for(cols);
-    int64_t groups = kBwdCtas * groups_per_cta(s.wpr);
-    if (rows < groups) groups = align_up((size_t)rows, groups_per_cta(s.wpr));
+    const Shape s = bwd_shape(cols, 3, rows <= kFewRows);
+    int64_t groups = kBwdCtas * s.groups;
+    if (rows < groups) groups = align_up((size_t)rows, (size_t)s.groups);
     *ws_bytes = align_up(sizeof(float) * (size_t)groups * (size_t)cols, 256);
     return SNIP_OK;
 }
@@ -718,31 +889,31 @@ extern "C" int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *t, void *ws, size_t ws
     a.rstd = t->rstd;
     a.dx = static_cast<uint16_t *>(t->dx);
     a.partials = t->dgain ? static_cast<float *>(ws) : nullptr;
-    a.ld_dy = t->ld_dy; a.ld_h = t->ld_h; a.ld_dresidual = t->ld_dresidual; a.ld_dx = t->ld_dx;
+    a.ld_dy = (int32_t)t->ld_dy; a.ld_h = (int32_t)t->ld_h; a.ld_dresidual = (int32_t)t->ld_dresidual; a.ld_dx = (int32_t)t->ld_dx;
     a.rows = (int32_t)t->rows;
     a.cols = (int32_t)t->cols;
     a.gain_f32 = t->gain_dtype == SNIP_OUT_FP32;
     a.inv_cols = (float)(1.0 / (double)t->cols);
-    const Shape s = shape_for(t->cols);
-    int64_t ctas = 0;
-    auto launch = [&](auto wpr, auto v, auto res) {
-        constexpr auto kernel = rmsnorm_bwd_kernel<wpr(), v(), res()>;
-        constexpr int smem = Ring<wpr(), v(), res() ? 3 : 2>::kBytes;
-        ctas = bwd_ctas(t->rows, wpr(), resident<kernel>(cta_threads(wpr()), smem));
-        if (ctas) kernel<<<(unsigned)ctas, cta_threads(wpr()), smem, st>>>(a);
+    const Shape s = bwd_shape(t->cols, t->dresidual ? 3 : 2, t->rows <= kFewRows);
+    a.wpr = s.wpr;
+    int64_t ctas = 0;   // 0: a CUDA call failed
+    auto launch = [&](auto v, auto threads, auto stages, auto res) {
+        constexpr auto kernel = rmsnorm_bwd_kernel<v(), threads(), stages(), res()>;
+        ctas = bwd_ctas(t->rows, s.groups, resident<kernel>(s.threads, s.smem, kMostSmem));
+        if (ctas) kernel<<<(unsigned)ctas, s.threads, s.smem, st>>>(a);
     };
-#define SNIP_LAUNCH(W, V)                                                                       \
-    if (s.wpr == W && s.v == V) {                                                               \
-        if (t->dresidual) launch(Int<W>{}, Int<V>{}, std::true_type{});                         \
-        else launch(Int<W>{}, Int<V>{}, std::false_type{});                                     \
+#define SNIP_LAUNCH(FORM, V, THREADS, STAGES)                                                   \
+    if (s.form == FORM) {                                                                       \
+        if (t->dresidual) launch(Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::true_type{});    \
+        else launch(Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::false_type{});                \
     }
-    SNIP_NORM_SHAPES(SNIP_LAUNCH)
+    SNIP_NORM_BWD_FORMS(SNIP_LAUNCH)
 #undef SNIP_LAUNCH
     SNIP_CUDA_TRY(cudaGetLastError());
     if (!ctas) return SNIP_ERR_CUDA;
     if (t->dgain) {
-        dgain_reduce_kernel<<<(unsigned)ceil_div(t->cols, 32), dim3(32, 32), 0, st>>>(a.partials, (int)(ctas * groups_per_cta(s.wpr)), a.cols, t->dgain, t->accumulate);
-        SNIP_CUDA_TRY(cudaGetLastError());
+        SNIP_CUDA_TRY(launch_behind(dgain_reduce_kernel, dim3((unsigned)ceil_div(t->cols, 32)), dim3(32, 32), 0, st, static_cast<const float *>(a.partials),
+                                    (int)(ctas * s.groups), (int)a.cols, t->dgain, (int)t->accumulate));
     }
     return SNIP_OK;
 }
