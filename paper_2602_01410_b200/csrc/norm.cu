@@ -333,181 +333,134 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_kernel(const NormArgs a)
     copies_wait<0>();
 }
 
-// Both quantized copies of y from h and rstd: 128x128 tiles, a thread owns 8x8 elements of one (dimensions are multiples of 64: all of
-// them or none).  Rows' maxima are combined over the 16 threads of a row group, columns' over the 16 row groups; the transposed codes
-// leave through shared memory.
-struct NormDualArgs {
+// The transposed copy, from h and rstd: codes on 128x1 tiles.  A CTA walks over 128x128 tiles; a warp takes 16 columns of 128 rows, a thread 8x8
+// elements of them (dimensions are multiples of 64: a thread has all of them or none), whose y stay in registers between the maximum and the
+// codes.  A column's 128 elements belong to 16 threads of the one warp, so that its maximum needs no barrier, and the eight codes that a thread
+// has of a column go straight to their place, 16 threads filling a 128-byte line.  A tile comes through shared memory, fetched in whole rows of
+// 256 bytes while the tile before it is worked on (fetched by the threads that use it, 32 bytes of a row at a time, 51 us instead of XX on
+// 16384 x 4096), its 16-byte pieces swizzled by the row group so that the 16 row groups of a warp read different banks; one barrier per tile.
+struct NormColsArgs {
     const uint16_t *h;
     const void *gain;
     const float *rstd;
-    uint8_t *codes, *codes_t;
-    float *scales, *scales_t;
+    uint8_t *codes_t;
+    float *scales_t;
     int32_t rows, cols, tiles_c, tiles, ld;
     int gain_f32;
 };
 constexpr int kTile = 128;
-constexpr int kDualThreads = 256;
-constexpr int kDualCtas = 3;
-
-struct DualShared {
-    uint4 slot[8][kDualThreads];                 // the thread's own eight vectors of eight elements
-    __align__(16) uint8_t stage[kTile * kTile];  // transposed codes
-    float col_max[8][kTile];
-    float col_scale[kTile];
-    float row_scale[kTile];
+constexpr int kColsThreads = 256;
+constexpr int kColsCtas = 2;
+struct ColsShared {
+    uint4 h[2][kTile * 16];
+    __align__(16) float rstd[2][kTile];
+    uint4 gain[2][32];
 };
 
-// FMT: format of the row-tile codes (BF16: none), FMT_T: of the transposed ones.
-template <int FMT, int FMT_T>
-__global__ void __launch_bounds__(kDualThreads, kDualCtas) rmsnorm_dual_kernel(const NormDualArgs a)
+template <int FMT>
+__global__ void __launch_bounds__(kColsThreads, kColsCtas) rmsnorm_cols_kernel(const NormColsArgs a)
 {
     extern __shared__ __align__(128) uint8_t raw[];
-    DualShared &m = *reinterpret_cast<DualShared *>(raw);
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31, warp = tid >> 5;
+    ColsShared &m = *reinterpret_cast<ColsShared *>(raw);
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, tx = lane & 1, ty = lane >> 1;
+    const int off_r = 8 * ty, off_c = 16 * warp + 8 * tx;   // of the thread's elements in a tile
+    const int piece = tid & 15, line = tid >> 4;            // what it fetches: 16 bytes of rows line, line + 16, ...
     // row and column of the tile, moved on without a division
     const int step_r = (int)gridDim.x / a.tiles_c, step_c = (int)gridDim.x % a.tiles_c;
-    auto advance = [&](int &r, int &c) {
-        r += step_r;
-        c += step_c;
-        if (c >= a.tiles_c) { c -= a.tiles_c; ++r; }
-    };
-    auto fetch = [&](int tile, int r, int c) {
-        if (tile < a.tiles && r * kTile + 8 * ty < a.rows && c * kTile + 8 * tx < a.cols) {
-            const uint16_t *p = a.h + (int64_t)(r * kTile + 8 * ty) * a.ld + c * kTile + 8 * tx;
+    auto fetch = [&](int buf, int tile, int r, int c) {
+        if (tile < a.tiles) {
+            const int row = r * kTile + line, col = c * kTile + 8 * piece;
+            const uint16_t *p = a.h + (int64_t)row * a.ld + col;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) copy_async(&m.slot[i][tid], p + (int64_t)i * a.ld);
+            for (int i = 0; i < 8; ++i, p += 16 * (int64_t)a.ld)
+                if (row + 16 * i < a.rows && col < a.cols) copy_async(&m.h[buf][(line + 16 * i) * 16 + (piece ^ ((line >> 3) + 2 * i))], p);
+            if (tid < 32) {
+                if (r * kTile + 4 * tid < a.rows) copy_async(reinterpret_cast<uint4 *>(&m.rstd[buf][4 * tid]), reinterpret_cast<const uint16_t *>(a.rstd + r * kTile + 4 * tid));
+            } else if (tid < 64) {
+                const int g = tid - 32, first = c * kTile + (a.gain_f32 ? 4 : 8) * g;
+                if (first < a.cols && (a.gain_f32 || g < 16))
+                    copy_async(&m.gain[buf][g], a.gain_f32 ? reinterpret_cast<const uint16_t *>(static_cast<const float *>(a.gain) + first) : static_cast<const uint16_t *>(a.gain) + first);
+            }
         }
         copies_commit();
     };
     asm volatile("griddepcontrol.wait;" ::: "memory");   // for the kernel that leaves h and rstd
-    int tr = (int)blockIdx.x / a.tiles_c, tc = (int)blockIdx.x % a.tiles_c;
-    fetch((int)blockIdx.x, tr, tc);
-    for (int tile = (int)blockIdx.x; tile < a.tiles; tile += (int)gridDim.x) {
-        int next_r = tr, next_c = tc;
-        advance(next_r, next_c);
-        const int row0 = tr * kTile + 8 * ty, col0 = tc * kTile + 8 * tx;
-        const bool ok = row0 < a.rows && col0 < a.cols;
-        Eight gain = zeros8();
-        float rstd[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) rstd[i] = 0.0f;
-        if (ok) {
-            gain = load_gain8(a.gain, a.gain_f32, col0);
-            const float4 p = __ldcg(reinterpret_cast<const float4 *>(a.rstd + row0)), q = __ldcg(reinterpret_cast<const float4 *>(a.rstd + row0) + 1);
-            rstd[0] = p.x; rstd[1] = p.y; rstd[2] = p.z; rstd[3] = p.w; rstd[4] = q.x; rstd[5] = q.y; rstd[6] = q.z; rstd[7] = q.w;
-        }
+    int tr = (int)blockIdx.x / a.tiles_c, tc = (int)blockIdx.x % a.tiles_c, buf = 0;
+    fetch(0, (int)blockIdx.x, tr, tc);
+    for (int tile = (int)blockIdx.x; tile < a.tiles; tile += (int)gridDim.x, buf ^= 1) {
+        int next_r = tr + step_r, next_c = tc + step_c;
+        if (next_c >= a.tiles_c) { next_c -= a.tiles_c; ++next_r; }
+        const int row = tr * kTile + off_r, col = tc * kTile + off_c;
+        const bool ok = row < a.rows && col < a.cols;
         copies_wait<0>();
-        float rmax[8], cmax[8];
+        __syncthreads();   // everybody's copies are here, and the other buffer has been read
+        fetch(buf ^ 1, tile + (int)gridDim.x, next_r, next_c);
+        Eight y[8];
+        if (ok) {
+            Eight gain;
+            if (a.gain_f32) {
+                const float4 g0 = *reinterpret_cast<const float4 *>(&m.gain[buf][off_c >> 2]), g1 = *reinterpret_cast<const float4 *>(&m.gain[buf][(off_c >> 2) + 1]);
+                gain = Eight{{make_float2(g0.x, g0.y), make_float2(g0.z, g0.w), make_float2(g1.x, g1.y), make_float2(g1.z, g1.w)}};
+            } else {
+                gain = unpack8(m.gain[buf][off_c >> 3]);
+            }
+            const float4 r0 = *reinterpret_cast<const float4 *>(&m.rstd[buf][off_r]), r1 = *reinterpret_cast<const float4 *>(&m.rstd[buf][off_r + 4]);
+            const float rstd[8] = {r0.x, r0.y, r0.z, r0.w, r1.x, r1.y, r1.z, r1.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) rmax[i] = cmax[i] = 0.0f;
-        if (ok) {   // (the slots of what a ragged tile lacks hold anything)
+            for (int i = 0; i < 8; ++i) y[i] = scaled8(unpack8(m.h[buf][(off_r + i) * 16 + ((off_c >> 3) ^ ty)]), rstd[i], gain);
+        } else {
 #pragma unroll
-        for (int p = 0; p < 8; p += 2) {
-            const Eight y0 = scaled8(unpack8(m.slot[p][tid]), rstd[p], gain), y1 = scaled8(unpack8(m.slot[p + 1][tid]), rstd[p + 1], gain);
-            rmax[p] = most8(y0);
-            rmax[p + 1] = most8(y1);
+            for (int i = 0; i < 8; ++i) y[i] = zeros8();
+        }
+        float most[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            most[2 * i] = fabsf(y[0].p[i].x);
+            most[2 * i + 1] = fabsf(y[0].p[i].y);
+#pragma unroll
+            for (int r = 1; r < 7; r += 2) {
+                most[2 * i] = fmaxf(fmaxf(most[2 * i], fabsf(y[r].p[i].x)), fabsf(y[r + 1].p[i].x));
+                most[2 * i + 1] = fmaxf(fmaxf(most[2 * i + 1], fabsf(y[r].p[i].y)), fabsf(y[r + 1].p[i].y));
+            }
+            most[2 * i] = fmaxf(most[2 * i], fabsf(y[7].p[i].x));
+            most[2 * i + 1] = fmaxf(most[2 * i + 1], fabsf(y[7].p[i].y));
+        }
+        // each step halves the number of columns a lane still looks after: lanes 4 q + tx and 4 q + 2 + tx end with column q's maximum
+#pragma unroll
+        for (int w = 4, off = 16; w > 0; w >>= 1, off >>= 1) {
+            const bool upper = (lane & off) != 0;
+#pragma unroll
+            for (int i = 0; i < w; ++i) {
+                const float give = upper ? most[i] : most[i + w], keep = upper ? most[i + w] : most[i];
+                most[i] = fmaxf(keep, __shfl_xor_sync(0xFFFFFFFFu, give, off));
+            }
+        }
+        most[0] = fmaxf(most[0], __shfl_xor_sync(0xFFFFFFFFu, most[0], 2));
+        const float own = tile_scale<FMT>(most[0], 0);
+        if ((lane & 2) == 0 && col < a.cols) a.scales_t[(int64_t)tr * a.cols + col + (lane >> 2)] = own;
+        Eight s;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s.p[i] = make_float2(__shfl_sync(0xFFFFFFFFu, own, 8 * i + tx), __shfl_sync(0xFFFFFFFFu, own, 8 * i + 4 + tx));
+        if (ok) {
+            constexpr int kPerByte = FMT == SNIP_FMT_FP4_E2M1 ? 2 : 1;
+            uint8_t *to = a.codes_t + ((int64_t)col * a.rows + row) / kPerByte;
+            const int64_t line = a.rows / kPerByte;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                cmax[2 * i] = fmaxf(fmaxf(cmax[2 * i], fabsf(y0.p[i].x)), fabsf(y1.p[i].x));
-                cmax[2 * i + 1] = fmaxf(fmaxf(cmax[2 * i + 1], fabsf(y0.p[i].y)), fabsf(y1.p[i].y));
-            }
-        }
-        }
-        if constexpr (FMT != SNIP_FMT_BF16) {
-            // rows: each step halves the number of rows a lane still looks after; lanes 2 q and 2 q + 1 of a half-warp end with row q's maximum
 #pragma unroll
-            for (int w = 4, off = 8; w > 0; w >>= 1, off >>= 1) {
-                const bool upper = (lane & off) != 0;
+                for (int r = 0; r < 8; ++r) y[r].p[i] = __fmul2_rn(y[r].p[i], s.p[i]);
 #pragma unroll
-                for (int i = 0; i < w; ++i) {
-                    const float give = upper ? rmax[i] : rmax[i + w], keep = upper ? rmax[i + w] : rmax[i];
-                    rmax[i] = fmaxf(keep, __shfl_xor_sync(0xFFFFFFFFu, give, off));
-                }
-            }
-            rmax[0] = fmaxf(rmax[0], __shfl_xor_sync(0xFFFFFFFFu, rmax[0], 1));
-            if ((lane & 1) == 0) {
-                const float s = tile_scale<FMT>(rmax[0], 0);
-                const int r = 8 * ty + ((lane >> 1) & 7), row = tr * kTile + r;
-                m.row_scale[r] = s;
-                if (row < a.rows) a.scales[(int64_t)tc * a.rows + row] = s;
-            }
-        }
-        // columns
+                for (int e = 0; e < 2; ++e, to += line) {
+                    uint32_t c[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) cmax[i] = fmaxf(cmax[i], __shfl_xor_sync(0xFFFFFFFFu, cmax[i], 16));
-        if (lane < 16) {
-            *reinterpret_cast<float4 *>(&m.col_max[warp][8 * tx]) = make_float4(cmax[0], cmax[1], cmax[2], cmax[3]);
-            *reinterpret_cast<float4 *>(&m.col_max[warp][8 * tx + 4]) = make_float4(cmax[4], cmax[5], cmax[6], cmax[7]);
-        }
-        __syncthreads();   // also: the previous tile's codes have left the stage
-        if (tid < kTile) {
-            float v = m.col_max[0][tid];
-#pragma unroll
-            for (int w = 1; w < 8; ++w) v = fmaxf(v, m.col_max[w][tid]);
-            const float s = tile_scale<FMT_T>(v, 0);
-            m.col_scale[tid] = s;
-            const int col = tc * kTile + tid;
-            if (col < a.cols) a.scales_t[(int64_t)tr * a.cols + col] = s;
-        }
-        __syncthreads();
-        Eight cs;
-        {
-            const float4 p = *reinterpret_cast<const float4 *>(&m.col_scale[8 * tx]), q = *reinterpret_cast<const float4 *>(&m.col_scale[8 * tx + 4]);
-            cs = {{make_float2(p.x, p.y), make_float2(p.z, p.w), make_float2(q.x, q.y), make_float2(q.z, q.w)}};
-        }
-        const int line = FMT == SNIP_FMT_FP4_E2M1 ? a.cols >> 1 : a.cols;
-        uint8_t *pc = FMT == SNIP_FMT_BF16 ? nullptr : a.codes + (int64_t)row0 * line + (FMT == SNIP_FMT_FP4_E2M1 ? col0 >> 1 : col0);
-        uint32_t ct[8][2];   // column i: codes of its eight rows (FP4: the first word)
-#pragma unroll
-        for (int p = 0; p < 8; p += 4) {
-            uint32_t part[2][8];
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                Eight y[2];
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    const int r = p + e + f;
-                    y[f] = scaled8(unpack8(m.slot[r][tid]), rstd[r], gain);
-                    if constexpr (FMT != SNIP_FMT_BF16)
-                        if (ok) store_codes8<FMT>(pc + (int64_t)r * line, y[f], m.row_scale[8 * ty + r]);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 t0 = __fmul2_rn(y[0].p[i], cs.p[i]), t1 = __fmul2_rn(y[1].p[i], cs.p[i]);
-                    if constexpr (FMT_T == SNIP_FMT_FP8_E4M3) {
-                        part[e >> 1][2 * i] = cvt_e4m3x2(t0.x, t1.x);
-                        part[e >> 1][2 * i + 1] = cvt_e4m3x2(t0.y, t1.y);
-                    } else {
-                        part[e >> 1][2 * i] = cvt_e2m1x2(t0.x, t1.x);
-                        part[e >> 1][2 * i + 1] = cvt_e2m1x2(t0.y, t1.y);
+                    for (int q = 0; q < 4; ++q) {
+                        const float lo = e ? y[2 * q].p[i].y : y[2 * q].p[i].x, hi = e ? y[2 * q + 1].p[i].y : y[2 * q + 1].p[i].x;
+                        c[q] = FMT == SNIP_FMT_FP8_E4M3 ? cvt_e4m3x2(lo, hi) : cvt_e2m1x2(lo, hi);
                     }
+                    if constexpr (FMT == SNIP_FMT_FP8_E4M3) *reinterpret_cast<uint2 *>(to) = make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
+                    else *reinterpret_cast<uint32_t *>(to) = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if constexpr (FMT_T == SNIP_FMT_FP8_E4M3) ct[i][p >> 2] = __byte_perm(part[0][i], part[1][i], 0x5410);
-                else ct[i][p >> 2] = __byte_perm(part[0][i], part[1][i], 0x0040);   // two bytes
-            }
-        }
-        fetch(tile + (int)gridDim.x, next_r, next_c);   // the slot has been read
-        // transposed codes: line = column of the tile, 128 (64) bytes each; 16-byte pieces swizzled by the line so that neither side conflicts
-        constexpr bool kFp8T = FMT_T == SNIP_FMT_FP8_E4M3;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int to = 8 * tx + i;
-            if constexpr (kFp8T) *reinterpret_cast<uint2 *>(&m.stage[to * 128 + ((ty >> 1) ^ (tx & 7)) * 16 + (ty & 1) * 8]) = make_uint2(ct[i][0], ct[i][1]);
-            else *reinterpret_cast<uint32_t *>(&m.stage[to * 64 + ((ty >> 2) ^ (tx & 3)) * 16 + (ty & 3) * 4]) = __byte_perm(ct[i][0], ct[i][1], 0x5410);
-        }
-        __syncthreads();
-        constexpr int kPieces = kFp8T ? 8 : 4, kRows = kFp8T ? 16 : 32;   // 16-byte pieces of a line, rows in one
-#pragma unroll
-        for (int j = 0; j < kTile * kPieces / kDualThreads; ++j) {
-            const int from = (j * kDualThreads + tid) / kPieces, piece = tid % kPieces;
-            const int row = tr * kTile + piece * kRows, col = tc * kTile + from;
-            if (col >= a.cols || row >= a.rows) continue;
-            const int64_t elem = (int64_t)col * a.rows + row;
-            *reinterpret_cast<uint4 *>(a.codes_t + (kFp8T ? elem : elem / 2)) =
-                *reinterpret_cast<const uint4 *>(&m.stage[from * (16 * kPieces) + (piece ^ ((from >> 3) & (kPieces - 1))) * 16]);
         }
         tr = next_r;
         tc = next_c;
@@ -769,7 +722,6 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     int rc = require_sm100();
     if (rc) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool dual = t->codes_t != nullptr;
     NormArgs a = {};
     a.x = static_cast<const uint16_t *>(t->x);
     a.residual = static_cast<const uint16_t *>(t->residual);
@@ -777,7 +729,7 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     a.h = static_cast<uint16_t *>(t->h);
     a.y = static_cast<uint16_t *>(t->y);
     a.rstd = t->rstd;
-    a.codes = dual ? nullptr : static_cast<uint8_t *>(t->codes);
+    a.codes = static_cast<uint8_t *>(t->codes);
     a.scales = t->scales;
     a.ld_x = (int32_t)t->ld_x; a.ld_residual = (int32_t)t->ld_residual; a.ld_h = (int32_t)t->ld_h; a.ld_y = (int32_t)t->ld_y;
     a.rows = (int32_t)t->rows;
@@ -808,35 +760,29 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
 #undef SNIP_LAUNCH
     SNIP_CUDA_TRY(cudaGetLastError());
     if (!n) return SNIP_ERR_CUDA;
-    if (!dual) return SNIP_OK;
-    NormDualArgs d = {};
+    if (!t->codes_t) return SNIP_OK;
+    NormColsArgs d = {};
     d.h = static_cast<const uint16_t *>(t->residual ? t->h : t->x);
     d.gain = t->gain;
     d.rstd = t->rstd;
-    d.codes = static_cast<uint8_t *>(t->codes);
-    d.scales = t->scales;
     d.codes_t = static_cast<uint8_t *>(t->codes_t);
     d.scales_t = t->scales_t;
     d.ld = (int32_t)(t->residual ? t->ld_h : t->ld_x);
-    d.rows = a.rows; d.cols = a.cols;
+    d.rows = a.rows;
+    d.cols = a.cols;
     d.tiles_c = (int32_t)ceil_div(t->cols, kTile);
     d.tiles = (int32_t)(d.tiles_c * ceil_div(t->rows, kTile));
     d.gain_f32 = a.gain_f32;
     cudaError_t e = cudaSuccess;
-    auto launch_dual = [&](auto fmt, auto fmt_t) {
-        constexpr auto kernel = rmsnorm_dual_kernel<fmt(), fmt_t()>;
-        constexpr int smem = (int)sizeof(DualShared);
-        n = resident<kernel>(kDualThreads, smem, smem);
+    auto launch_cols = [&](auto fmt) {
+        constexpr auto kernel = rmsnorm_cols_kernel<fmt()>;
+        constexpr int smem = (int)sizeof(ColsShared);
+        n = resident<kernel>(kColsThreads, smem, smem);
         const int64_t cap = (int64_t)n * gemm_sm_count();
-        if (n) e = launch_behind(kernel, dim3((unsigned)(d.tiles < cap ? d.tiles : cap)), dim3(kDualThreads), smem, st, d);
+        if (n) e = launch_behind(kernel, dim3((unsigned)(d.tiles < cap ? d.tiles : cap)), dim3(kColsThreads), smem, st, d);
     };
-    auto with_fmt_t = [&](auto fmt) {
-        if (t->fmt_t == SNIP_FMT_FP8_E4M3) launch_dual(fmt, Int<SNIP_FMT_FP8_E4M3>{});
-        else launch_dual(fmt, Int<SNIP_FMT_FP4_E2M1>{});
-    };
-    if (!d.codes) with_fmt_t(Int<SNIP_FMT_BF16>{});
-    else if (t->fmt == SNIP_FMT_FP8_E4M3) with_fmt_t(Int<SNIP_FMT_FP8_E4M3>{});
-    else with_fmt_t(Int<SNIP_FMT_FP4_E2M1>{});
+    if (t->fmt_t == SNIP_FMT_FP8_E4M3) launch_cols(Int<SNIP_FMT_FP8_E4M3>{});
+    else launch_cols(Int<SNIP_FMT_FP4_E2M1>{});
     SNIP_CUDA_TRY(e);
     return n ? SNIP_OK : SNIP_ERR_CUDA;
 }
