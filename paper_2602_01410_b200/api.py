@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import bisect
 import ctypes
+import functools
 import os
 
 import torch
@@ -549,14 +550,21 @@ def _call_on(dev, fn, call, args):
 _BF16, _F32, _U8 = torch.bfloat16, torch.float32, torch.uint8
 
 
-def _matrix(t, shape, dev, name):
-    """Checks a bf16 matrix of `shape` on device `dev`; its row stride."""
-    if t.dtype is not _BF16 or t.shape != shape or t.get_device() != dev:
-        raise ValueError(f"{name}: a bf16 tensor of shape {tuple(shape)} on CUDA device {dev} is wanted")
+def _rows_apart(t, shape, name):
+    """Row stride of a bf16 matrix of `shape`."""
+    if t.dtype is not _BF16:
+        raise ValueError(f"{name}: a bf16 tensor is wanted")
     ld, step = t.stride()
     if step != 1 and shape[1] != 1:
         raise ValueError(f"{name}: the elements of a row have to be adjacent")
     return ld if shape[0] > 1 else shape[1]   # a single row's stride says nothing
+
+
+def _matrix(t, shape, dev, name):
+    """Checks a bf16 matrix of `shape` on device `dev`; its row stride."""
+    if t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{name}: a bf16 tensor of shape {tuple(shape)} on CUDA device {dev} is wanted")
+    return _rows_apart(t, shape, name)
 
 
 def _vector(t, n, dtype, dev, name):
@@ -630,7 +638,7 @@ def snip_rmsnorm_fwd(x: torch.Tensor, gain: torch.Tensor, eps: float, *, residua
         h = None   # what an earlier call returned for h
     a = RmsNorm()
     a.rows, a.cols, a.eps = rows, cols, eps
-    a.ld_x, a.x = _matrix(x, shape, dev, "x"), x.data_ptr()
+    a.ld_x, a.x = _rows_apart(x, shape, "x"), x.data_ptr()
     a.gain, a.gain_dtype = _gain(gain, cols, dev)
     if residual is not None:
         _require(h is not None, "out: the sum with a residual needs h")
@@ -654,6 +662,7 @@ def snip_rmsnorm_fwd(x: torch.Tensor, gain: torch.Tensor, eps: float, *, residua
     return {"h": x if h is None else h, "y": y, "rstd": rstd, "codes": codes, "scales": scales, "codes_t": codes_t, "scales_t": scales_t}
 
 
+@functools.lru_cache(maxsize=256)   # of the sizes alone
 def snip_rmsnorm_bwd_workspace(rows, cols):
     n = ctypes.c_size_t()
     _check("snip_rmsnorm_bwd_workspace", _lib.snip_rmsnorm_bwd_workspace(rows, cols, ctypes.byref(n)))
@@ -676,7 +685,7 @@ def snip_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd
         dgain = torch.empty(cols, dtype=_F32, device=dy.device)
     a = RmsNormBwd()
     a.rows, a.cols, a.accumulate = rows, cols, 1 if accumulate else 0
-    a.ld_dy, a.dy = _matrix(dy, shape, dev, "dy"), dy.data_ptr()
+    a.ld_dy, a.dy = _rows_apart(dy, shape, "dy"), dy.data_ptr()
     a.ld_h, a.h = _matrix(h, shape, dev, "h"), h.data_ptr()
     a.ld_dx, a.dx = _matrix(dx, shape, dev, "dx"), dx.data_ptr()
     if dresidual is not None:

@@ -367,7 +367,9 @@ __global__ void __launch_bounds__(kColsThreads, kColsCtas) rmsnorm_cols_kernel(c
     const int piece = tid & 15, line = tid >> 4;            // what it fetches: 16 bytes of rows line, line + 16, ...
     // row and column of the tile, moved on without a division
     const int step_r = (int)gridDim.x / a.tiles_c, step_c = (int)gridDim.x % a.tiles_c;
+    const int last_r = a.tiles / a.tiles_c - 1;   // from the last tile row back: what of h is still in the L2 cache is read from there
     auto fetch = [&](int buf, int tile, int r, int c) {
+        r = last_r - r;
         if (tile < a.tiles) {
             const int row = r * kTile + line, col = c * kTile + 8 * piece;
             const uint16_t *p = a.h + (int64_t)row * a.ld + col;
@@ -385,10 +387,11 @@ __global__ void __launch_bounds__(kColsThreads, kColsCtas) rmsnorm_cols_kernel(c
         copies_commit();
     };
     asm volatile("griddepcontrol.wait;" ::: "memory");   // for the kernel that leaves h and rstd
-    int tr = (int)blockIdx.x / a.tiles_c, tc = (int)blockIdx.x % a.tiles_c, buf = 0;
-    fetch(0, (int)blockIdx.x, tr, tc);
+    int done = (int)blockIdx.x / a.tiles_c, tc = (int)blockIdx.x % a.tiles_c, buf = 0;
+    fetch(0, (int)blockIdx.x, done, tc);
     for (int tile = (int)blockIdx.x; tile < a.tiles; tile += (int)gridDim.x, buf ^= 1) {
-        int next_r = tr + step_r, next_c = tc + step_c;
+        const int tr = last_r - done;
+        int next_r = done + step_r, next_c = tc + step_c;
         if (next_c >= a.tiles_c) { next_c -= a.tiles_c; ++next_r; }
         const int row = tr * kTile + off_r, col = tc * kTile + off_c;
         const bool ok = row < a.rows && col < a.cols;
@@ -462,7 +465,7 @@ __global__ void __launch_bounds__(kColsThreads, kColsCtas) rmsnorm_cols_kernel(c
                 }
             }
         }
-        tr = next_r;
+        done = next_r;
         tc = next_c;
     }
     copies_wait<0>();
