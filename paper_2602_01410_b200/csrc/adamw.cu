@@ -68,21 +68,21 @@ __host__ __device__ inline Hyper hyper(double lr, double beta1, double beta2, in
 }
 
 // Stochastic rounding of a pair of values to E4M3, by one 32-bit word of the generator (its low half for the first): with a = |t|, lo <= a < hi
-// the neighbouring grid points and u the 16-bit uniform, hi iff (a - lo)/(hi - lo) > (u + 1/2)/2^16.  On the bits of 64 a, as for E2M1: from
-// 1 up a grid point has 20 zero bits at its end, and their value f exceeds 16 u + 8 iff f + 16 (65535 - u) + 7 carries out of them; below,
-// the same holds for 64 a + 1, rounded upwards.  t comes from a block scaled by its own maximum: it passes 448 by a few last places at
-// most, which leave the largest addend 9 units short of a carry.  SIGNED = false: t >= 0.
+// the neighbouring grid points and u the 16-bit uniform, hi iff (a - lo)/(hi - lo) > (u + 1/2)/2^16.  On the bits, as for E2M1: from 2^-6 up a
+// grid point has 20 zero bits at its end, and their value f exceeds 16 u + 8 iff f + 16 (65535 - u) + 7 carries out of them; below, the same
+// holds for a + 2^-6, rounded upwards.  t comes from a block scaled by its own maximum: it passes 448 by a few last places at most, which
+// leave the largest addend 9 units short of a carry.  SIGNED = false: t >= 0.
 template <bool SIGNED>
 __device__ __forceinline__ float2 sr_e4m3x2(const float2 t, uint32_t w)
 {
-    const float2 b = __fmul2_rn(t, make_float2(64.0f, 64.0f)), a = SIGNED ? make_float2(fabsf(b.x), fabsf(b.y)) : b;
-    float2 off;   // 1 below 1, else 0, on the FMA pipe (a comparison and a selection per value on the integer pipe: 602 against 598 us)
-    asm("fma.rn.sat.f32 %0, %1, 0fFB800000, 0f7B800000;" : "=f"(off.x) : "f"(a.x));
-    asm("fma.rn.sat.f32 %0, %1, 0fFB800000, 0f7B800000;" : "=f"(off.y) : "f"(a.y));
-    const float2 s = __fadd2_ru(a, off);
+    const float2 a = SIGNED ? make_float2(fabsf(t.x), fabsf(t.y)) : t;
+    float2 off;   // 1 below 2^-6, else 0: 2^120 - 2^126 a, clamped to [0, 1], on the FMA pipe
+    asm("fma.rn.sat.f32 %0, %1, 0fFE800000, 0f7B800000;" : "=f"(off.x) : "f"(a.x));
+    asm("fma.rn.sat.f32 %0, %1, 0fFE800000, 0f7B800000;" : "=f"(off.y) : "f"(a.y));
+    const float2 s = __ffma2_ru(off, make_float2(0.015625f, 0.015625f), a);
     const uint32_t r0 = ((~w << 4) & 0xFFFF0u) | 7u, r1 = ((~w >> 12) & 0xFFFF0u) | 7u;
     const float2 q = make_float2(__uint_as_float((__float_as_uint(s.x) + r0) & 0xFFF00000u), __uint_as_float((__float_as_uint(s.y) + r1) & 0xFFF00000u));
-    const float2 v = __ffma2_rn(q, make_float2(0.015625f, 0.015625f), __fmul2_rn(off, make_float2(-0.015625f, -0.015625f)));
+    const float2 v = __ffma2_rn(off, make_float2(-0.015625f, -0.015625f), q);
     return SIGNED ? make_float2(copysignf(v.x, t.x), copysignf(v.y, t.y)) : v;
 }
 // ... to bf16 bits, packed: the low 16 bits f exceed u + 1/2 iff f + 65535 - u carries.
@@ -399,8 +399,8 @@ __device__ __forceinline__ int locate(const Table<CAP> &a, uint32_t chunk, Chunk
 }
 
 // CTAs per SM that the registers are cut for.  A 7B block (202 M elements) in us, at five / six / seven: 8-bit states to nearest 544 / 569 / 567
-// with binary32 weights, 377 / 354 / 340 with bf16 ones; stochastic 609 / 598 / 580 and 695 / 722 / 739 (two generator calls per four elements:
-// fewer registers spill).  Binary32 states: six keep 24 warps of one block each in flight; two blocks per warp or more warps are no faster.
+// with binary32 weights, 377 / 354 / 340 with bf16 ones; stochastic (a long run, at the power limit) 630 / 624 / 616 and 684 / 710 / 718 (two
+// generator calls per four elements: fewer registers spill).  Binary32 states: six keep 24 warps of one block each in flight; two blocks per warp or more warps are no faster.
 constexpr int resident_ctas(bool p16, bool bits8, bool sr)
 {
     return !bits8 ? 6 : p16 == sr ? 5 : 7;
