@@ -466,10 +466,10 @@ int snip_adamw_sensitivity(const float *m, const float *v, const void *g, int g_
  * quantizing y; the codes of `codes` do not depend on which other outputs are asked for).
  * rows: any number >= 0 (0: nothing is done); cols: a multiple of 8 up to 32768; a last tile is as long as what is left.
  * With codes_t both must be multiples of 64, as the products behind it want them.  FP4 code buffers carry the slack of
- * snip_quantize_sizes.  Strides: multiples of 8, >= cols.
- * Inputs finite, with a mean of h^2 that binary32 holds; eps > 0.  Other outputs must overlap neither each other nor an input.
- * No workspace.  Bytes per element: 2 (x) + 4 (residual, h) + 2 (y) + code and scale bytes of each copy; with
- * codes_t h is read once more where it does not come out of the L2 cache.
+ * snip_quantize_sizes.  Strides: multiples of 8, >= cols, below 2^31.
+ * Inputs finite, with a sum of h^2 over a row that binary32 holds; eps > 0.  Other outputs must overlap neither each other nor an input
+ * (SNIP_ERR_ARG where the same address is given twice).  No workspace.  Bytes per element: 2 (x) + 4 (residual, h) + 2 (y) + code and
+ * scale bytes of each copy; with codes_t, which a second kernel makes, h is read once more.
  */
 typedef struct {
     const void *x;        /* bf16 [rows][ld_x] */
@@ -534,7 +534,7 @@ int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *args_host, void *ws, size_t ws_by
  * 16-bit uniform of element i for m in bits [16 (i%2), +16) of output word i/2, for v in word 2 + i/2; kind 1: a bf16 param's, as for m.
  * (Rounded to nearest, an 8-bit v stops moving once a step changes it by less than half a code; long runs want stochastic rounding.)
  * step >= 1 counts this step.  step_device, lr_device (device, may be NULL) take the place of step and lr: a captured graph then reads
- * the current values at each replay.  grad_scale (device, may be NULL = 1): inverse loss scale, clipping factor.
+ * the current values at each replay (a *step_device below 1 counts as 1).  grad_scale (device, may be NULL = 1): inverse loss scale, clipping factor.
  * eps: a normal binary32 number.  The root of a v below 2^-126 comes out too small (0 stays 0).
  * Alignment: 16 bytes, scales 4.  n: any, 0 included.  Inputs finite.  The tensors must not overlap each other (what is written is
  * written once).  No workspace; one launch per 448 tensors, read and written once per element.

@@ -49,6 +49,7 @@ struct Common {
     const int64_t *step_device;
     const float *lr_device, *grad_scale;
     uint32_t k0, k1;                     // the generator's key
+    int64_t step_host;
     uint32_t step;
     uint32_t chunks;
     int32_t count, first_tensor;
@@ -415,7 +416,8 @@ __global__ void __launch_bounds__(kThreads, resident_ctas(P_BF16, BITS8, SR)) ad
     s.h = c.h;
     uint32_t step = c.step;
     if (c.step_device || c.lr_device) {
-        const int64_t t = c.step_device ? *c.step_device : (int64_t)c.step;
+        int64_t t = c.step_device ? *c.step_device : c.step_host;
+        t = t < 1 ? 1 : t;
         if (threadIdx.x == 0) shared_hyper = hyper(c.lr_device ? (double)*c.lr_device : c.lr, c.beta1, c.beta2, t);
         __syncthreads();
         s.h = shared_hyper;
@@ -553,6 +555,7 @@ extern "C" int snip_adamw_step(const snip_adamw_tensor_t *ts, int64_t count, con
     if (!a->step_device) c.h = hyper(a->lr, a->beta1, a->beta2, a->step);
     c.step_device = a->step_device; c.lr_device = a->lr_device; c.grad_scale = a->grad_scale;
     c.k0 = (uint32_t)a->seed; c.k1 = (uint32_t)(a->seed >> 32);
+    c.step_host = a->step;
     c.step = (uint32_t)a->step;
     c.b1 = (float)a->beta1; c.omb1 = (float)(1.0 - a->beta1);
     c.b2 = (float)a->beta2; c.omb2 = (float)(1.0 - a->beta2);

@@ -653,17 +653,21 @@ int resident(int threads, int smem, int most_smem)
 {
     static std::atomic<uint64_t> allowed{0};   // a bit per device
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    auto failed = [](const char *what) {
+        set_last_error(what, cudaGetLastError());
+        return 0;
+    };
+    if (cudaGetDevice(&dev) != cudaSuccess) return failed("cudaGetDevice");
     const uint64_t bit = 1ull << (dev & 63);
     if (!(allowed.load(std::memory_order_relaxed) & bit) || dev > 63) {
-        if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem) != cudaSuccess) return 0;
+        if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most_smem) != cudaSuccess) return failed("cudaFuncSetAttribute");
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
     // by threads: the shared memory goes with them
     static std::atomic<int> known[33];
     int n = known[threads / 32].load(std::memory_order_relaxed);
     if (n == 0) {
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, Kernel, threads, smem) != cudaSuccess || n < 1) return 0;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, Kernel, threads, smem) != cudaSuccess || n < 1) return failed("cudaOccupancyMaxActiveBlocksPerMultiprocessor");
         known[threads / 32].store(n, std::memory_order_relaxed);
     }
     return n;
@@ -722,6 +726,15 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     const void *all[] = {t->x, t->residual, t->gain, t->h, t->y, t->rstd, t->codes, t->scales, t->codes_t, t->scales_t};
     for (const void *p : all)
         if (!aligned16(p)) return SNIP_ERR_ALIGN;
+    // of the outputs only h may be an input, row for row
+    if ((t->h && t->h == t->x && t->ld_h != t->ld_x) || (t->h && t->h == t->residual && t->ld_h != t->ld_residual)) return SNIP_ERR_ARG;
+    const void *out[] = {t->h, t->y, t->rstd, t->codes, t->scales, t->codes_t, t->scales_t}, *in[] = {t->x, t->residual, t->gain};
+    for (int i = 0; i < 7; ++i) {
+        for (int j = i + 1; out[i] && j < 7; ++j)
+            if (out[i] == out[j]) return SNIP_ERR_ARG;
+        for (int j = 0; out[i] && j < 3; ++j)
+            if (out[i] == in[j] && (i > 0 || j == 2)) return SNIP_ERR_ARG;
+    }
     int rc = require_sm100();
     if (rc) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -822,6 +835,10 @@ extern "C" int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *t, void *ws, size_t ws
     const void *all[] = {t->dy, t->h, t->gain, t->rstd, t->dresidual, t->dx, t->dgain, t->dgain ? ws : nullptr};
     for (const void *p : all)
         if (!aligned16(p)) return SNIP_ERR_ALIGN;
+    if ((t->dx == t->dy && t->ld_dx != t->ld_dy) || (t->dx == t->dresidual && t->ld_dx != t->ld_dresidual) || t->dx == t->h || t->dx == t->gain ||
+        t->dx == t->rstd || (t->dgain && (t->dgain == t->gain || t->dgain == t->dx || t->dgain == t->rstd || t->dgain == t->dy || t->dgain == t->h ||
+                                          t->dgain == t->dresidual || t->dgain == ws)))
+        return SNIP_ERR_ARG;
     if (t->dgain) {
         size_t need = 0;
         int rc = snip_rmsnorm_bwd_workspace(t->rows, t->cols, &need);

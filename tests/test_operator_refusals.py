@@ -37,11 +37,35 @@ def test_norm_forward(api):
         assert fwd(api, **{name: P + 8}) == api.ERR_ALIGN, name
     for kw in (dict(residual=P + 2, h=Q), dict(residual=P, h=Q + 4), dict(codes=Q + 8, scales=Q), dict(codes=Q, scales=Q + 4), dict(codes_t=Q, scales_t=Q + 8, rstd=Q)):
         assert fwd(api, **kw) == api.ERR_ALIGN, kw
+    assert fwd(api, ld_x=1 << 31) == api.ERR_SHAPE
     assert fwd(api, rows=0) == api.OK      # nothing to do
 
 
+def test_norm_forward_refuses_one_address_for_two(api):
+    full = dict(residual=0x30000, h=0x40000, rstd=0x50000, codes=0x60000, scales=0x70000, codes_t=0x80000, scales_t=0x90000, x=0xA0000, gain=0xB0000, y=0xC0000)
+    outs = ("h", "y", "rstd", "codes", "scales", "codes_t", "scales_t")
+    for i, a in enumerate(outs):
+        for b in outs[i + 1:]:
+            assert fwd(api, **{**full, a: full[b]}) == api.ERR_ARG, (a, b)
+        for b in ("x", "residual", "gain"):
+            if a != "h" or b == "gain":
+                assert fwd(api, **{**full, a: full[b]}) == api.ERR_ARG, (a, b)
+    # the sum in place: with the same stride only
+    assert fwd(api, **{**full, "h": full["x"], "ld_x": 136}) == api.ERR_ARG
+    assert fwd(api, **{**full, "h": full["residual"], "ld_residual": 136}) == api.ERR_ARG
+
+
+def test_norm_backward_refuses_one_address_for_two(api):
+    full = dict(dy=0x30000, h=0x40000, gain=0x50000, rstd=0x60000, dresidual=0x70000, dx=0x80000, dgain=0x90000)
+    for a, b in (("dx", "h"), ("dx", "gain"), ("dx", "rstd"), ("dgain", "gain"), ("dgain", "rstd"), ("dgain", "dy"), ("dgain", "h"), ("dgain", "dresidual"), ("dgain", "dx")):
+        assert bwd(api, **{**full, a: full[b]}) == api.ERR_ARG, (a, b)
+    assert bwd(api, ws=full["dgain"], **full) == api.ERR_ARG
+    assert bwd(api, **{**full, "dx": full["dy"], "ld_dy": 136}) == api.ERR_ARG
+    assert bwd(api, **{**full, "dx": full["dresidual"], "ld_dresidual": 136}) == api.ERR_ARG
+
+
 def bwd(api, ws=P, size=1 << 40, **kw):
-    a = api.RmsNormBwd(dy=P, h=P, gain=P, rstd=P, dx=Q, dgain=Q, rows=128, cols=128, ld_dy=128, ld_h=128, ld_dresidual=128, ld_dx=128, gain_dtype=1)
+    a = api.RmsNormBwd(dy=P, h=P, gain=P, rstd=P, dx=Q, dgain=Q + 0x8000, rows=128, cols=128, ld_dy=128, ld_h=128, ld_dresidual=128, ld_dx=128, gain_dtype=1)
     for k, v in kw.items():
         setattr(a, k, v)
     return api._lib.snip_rmsnorm_bwd(ctypes.byref(a), ws, size, None)
@@ -54,7 +78,7 @@ def test_norm_backward(api):
     assert bwd(api, gain_dtype=-1) == api.ERR_ARG
     for kw in (dict(rows=-1), dict(cols=12), dict(cols=0), dict(ld_dy=8), dict(ld_h=130), dict(ld_dx=0), dict(dresidual=P, ld_dresidual=100)):
         assert bwd(api, **kw) == api.ERR_SHAPE, kw
-    for kw in (dict(dy=P + 8), dict(h=P + 2), dict(gain=P + 4), dict(rstd=P + 4), dict(dx=Q + 8), dict(dgain=Q + 4), dict(dresidual=P + 8), dict(ws=P + 8)):
+    for kw in (dict(dy=P + 8), dict(h=P + 2), dict(gain=P + 4), dict(rstd=P + 4), dict(dx=Q + 8), dict(dgain=Q + 0x8004), dict(dresidual=P + 8), dict(ws=P + 8)):
         assert bwd(api, **kw) == api.ERR_ALIGN, kw
     need = api.snip_rmsnorm_bwd_workspace(128, 128)
     assert need >= 4 * 128 and need % 256 == 0
