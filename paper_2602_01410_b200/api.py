@@ -11,6 +11,7 @@ import bisect
 import ctypes
 import functools
 import os
+import struct
 
 import torch
 
@@ -126,11 +127,12 @@ def _load():
     lib.snip_layer_stats_workspace.argtypes = [i64, i64, i64, psz]
     lib.snip_adamw_sensitivity_workspace.argtypes = [i64, psz]
     lib.snip_adamw_sensitivity.argtypes = [vp, vp, vp, i32, i64, ctypes.c_float, ctypes.c_float, ctypes.c_float, vp, vp, sz, vp]
-    lib.snip_rmsnorm_fwd.argtypes = [ctypes.POINTER(RmsNorm), vp]
+    # (a RmsNorm, RmsNormBwd or Adamw by reference, or its bytes)
+    lib.snip_rmsnorm_fwd.argtypes = [vp, vp]
     lib.snip_rmsnorm_bwd_workspace.argtypes = [i64, i64, psz]
-    lib.snip_rmsnorm_bwd.argtypes = [ctypes.POINTER(RmsNormBwd), vp, sz, vp]
+    lib.snip_rmsnorm_bwd.argtypes = [vp, vp, sz, vp]
     lib.snip_adamw_state_sizes.argtypes = [i64, i32, psz, psz]
-    lib.snip_adamw_step.argtypes = [ctypes.POINTER(AdamwTensor), i64, ctypes.POINTER(Adamw), vp]
+    lib.snip_adamw_step.argtypes = [ctypes.POINTER(AdamwTensor), i64, vp, vp]
     dbl = ctypes.c_double
     lib.snip_loss_divergence.restype = dbl
     lib.snip_loss_divergence.argtypes = [dbl, dbl, i64, i64, dbl, dbl, i64, dbl]
@@ -587,6 +589,10 @@ def _cuda_device(t, name):
     return dev
 
 
+# a call's structure, as its bytes (filling a ctypes structure field by field takes three times as long)
+_RMSNORM_ARGS = struct.Struct("=10Q6qf3i").pack        # RmsNorm
+_RMSNORM_BWD_ARGS = struct.Struct("=7Q6q2i").pack      # RmsNormBwd
+_ADAMW_ARGS = struct.Struct("=4dq4Q4i").pack            # Adamw
 _RMSNORM_OUTPUTS = frozenset(("h", "y", "rstd", "codes", "scales", "codes_t", "scales_t"))
 _QUANT = (FMT_FP8_E4M3, FMT_FP4_E2M1)
 
@@ -636,28 +642,27 @@ def snip_rmsnorm_fwd(x: torch.Tensor, gain: torch.Tensor, eps: float, *, residua
     h, y, rstd, codes, scales, codes_t, scales_t = get("h"), get("y"), get("rstd"), get("codes"), get("scales"), get("codes_t"), get("scales_t")
     if residual is None and h is x:
         h = None   # what an earlier call returned for h
-    a = RmsNorm()
-    a.rows, a.cols, a.eps = rows, cols, eps
-    a.ld_x, a.x = _rows_apart(x, shape, "x"), x.data_ptr()
-    a.gain, a.gain_dtype = _gain(gain, cols, dev)
+    ld_x, (p_gain, gain_dtype) = _rows_apart(x, shape, "x"), _gain(gain, cols, dev)
+    p_res = ld_res = p_h = ld_h = p_y = ld_y = p_rstd = p_codes = p_scales = p_codes_t = p_scales_t = 0
     if residual is not None:
-        _require(h is not None, "out: the sum with a residual needs h")
-        a.ld_residual, a.residual = _matrix(residual, shape, dev, "residual"), residual.data_ptr()
-        a.ld_h, a.h = _matrix(h, shape, dev, "h"), h.data_ptr()
-    else:
-        _require(h is None, "out: h goes with a residual")
+        if h is None:
+            raise ValueError("out: the sum with a residual needs h")
+        ld_res, p_res = _matrix(residual, shape, dev, "residual"), residual.data_ptr()
+        ld_h, p_h = _matrix(h, shape, dev, "h"), h.data_ptr()
+    elif h is not None:
+        raise ValueError("out: h goes with a residual")
     if y is not None:
-        a.ld_y, a.y = _matrix(y, shape, dev, "y"), y.data_ptr()
+        ld_y, p_y = _matrix(y, shape, dev, "y"), y.data_ptr()
     if rstd is not None:
-        a.rstd = _vector(rstd, rows, _F32, dev, "rstd")
+        p_rstd = _vector(rstd, rows, _F32, dev, "rstd")
     if (codes is None) != (scales is None) or (codes_t is None) != (scales_t is None):
         raise ValueError("out: codes and scales go together")
     if codes is not None:
-        a.codes, a.scales = _copy_of(codes, scales, fmt, rows, cols, dev, "codes")
-        a.fmt = fmt
+        p_codes, p_scales = _copy_of(codes, scales, fmt, rows, cols, dev, "codes")
     if codes_t is not None:
-        a.codes_t, a.scales_t = _copy_of(codes_t, scales_t, fmt_t, cols, rows, dev, "codes_t")
-        a.fmt_t = fmt_t
+        p_codes_t, p_scales_t = _copy_of(codes_t, scales_t, fmt_t, cols, rows, dev, "codes_t")
+    a = _RMSNORM_ARGS(x.data_ptr(), p_res, p_gain, p_h, p_y, p_rstd, p_codes, p_scales, p_codes_t, p_scales_t, rows, cols, ld_x, ld_res, ld_h, ld_y, eps,
+                      gain_dtype, fmt or 0, fmt_t or 0)
     _call_on(dev, "snip_rmsnorm_fwd", _lib.snip_rmsnorm_fwd, (a,))
     return {"h": x if h is None else h, "y": y, "rstd": rstd, "codes": codes, "scales": scales, "codes_t": codes_t, "scales_t": scales_t}
 
@@ -683,22 +688,22 @@ def snip_rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd
     if dgain is None and want_dgain:
         _require(not accumulate, "accumulate: needs the dgain to add to")
         dgain = torch.empty(cols, dtype=_F32, device=dy.device)
-    a = RmsNormBwd()
-    a.rows, a.cols, a.accumulate = rows, cols, 1 if accumulate else 0
-    a.ld_dy, a.dy = _rows_apart(dy, shape, "dy"), dy.data_ptr()
-    a.ld_h, a.h = _matrix(h, shape, dev, "h"), h.data_ptr()
-    a.ld_dx, a.dx = _matrix(dx, shape, dev, "dx"), dx.data_ptr()
+    ld_dy, ld_h, ld_dx = _rows_apart(dy, shape, "dy"), _matrix(h, shape, dev, "h"), _matrix(dx, shape, dev, "dx")
+    p_res = ld_res = p_dgain = at = size = 0
     if dresidual is not None:
-        a.ld_dresidual, a.dresidual = _matrix(dresidual, shape, dev, "dresidual"), dresidual.data_ptr()
-    a.gain, a.gain_dtype = _gain(gain, cols, dev)
-    a.rstd = _vector(rstd, rows, _F32, dev, "rstd")
-    at, size = None, 0
+        ld_res, p_res = _matrix(dresidual, shape, dev, "dresidual"), dresidual.data_ptr()
+    p_gain, gain_dtype = _gain(gain, cols, dev)
+    p_rstd = _vector(rstd, rows, _F32, dev, "rstd")
     if dgain is not None:
-        a.dgain = _vector(dgain, cols, _F32, dev, "dgain")
+        p_dgain = _vector(dgain, cols, _F32, dev, "dgain")
         if ws is None:
-            ws = torch.empty(snip_rmsnorm_bwd_workspace(rows, cols), dtype=_U8, device=dy.device)
-        size = ws.numel() * ws.element_size()
-        at = _vector(ws, ws.numel(), ws.dtype, dev, "ws")
+            size = snip_rmsnorm_bwd_workspace(rows, cols)
+            ws = torch.empty(size, dtype=_U8, device=dy.device)
+            at = ws.data_ptr()
+        else:
+            size = ws.numel() * ws.element_size()
+            at = _vector(ws, ws.numel(), ws.dtype, dev, "ws")
+    a = _RMSNORM_BWD_ARGS(dy.data_ptr(), h.data_ptr(), p_gain, p_rstd, p_res, dx.data_ptr(), p_dgain, rows, cols, ld_dy, ld_h, ld_res, ld_dx, gain_dtype, 1 if accumulate else 0)
     _call_on(dev, "snip_rmsnorm_bwd", _lib.snip_rmsnorm_bwd, (a, at, size))
     return dx, dgain
 
@@ -774,8 +779,8 @@ def snip_adamw_step(tensors: AdamwTensors, lr, beta1: float, beta2: float, eps: 
         if t is not None:
             _vector(t, 1, dtype, tensors.device, name)
     _require(0 <= seed < 1 << 64, "seed: 64 bits")
-    a = Adamw(0.0 if lr_dev is not None else lr, beta1, beta2, eps, 0 if step_dev is not None else step, _p(step_dev), _p(lr_dev), _p(grad_scale), seed,
-              tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, rounding)
+    a = _ADAMW_ARGS(0.0 if lr_dev is not None else lr, beta1, beta2, eps, 0 if step_dev is not None else step, _p(step_dev) or 0, _p(lr_dev) or 0,
+                    _p(grad_scale) or 0, seed, tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, rounding)
     _call_on(tensors.device, "snip_adamw_step", _lib.snip_adamw_step, (tensors.table, tensors.count, a))
 
 

@@ -198,3 +198,13 @@ def test_binding_refuses_overlapping_and_mismatched_lists(api):
     for kw in (dict(seed=-1), dict(seed=1 << 64), dict(grad_scale=torch.ones(1))):
         with pytest.raises(ValueError):
             api.snip_adamw_step(ok, 1e-3, 0.9, 0.95, 1e-8, 1, **kw)
+
+
+def test_packed_arguments_have_the_structures_layout(api):
+    # what the binding packs is read back field by field through the structure
+    a = api.RmsNorm.from_buffer_copy(api._RMSNORM_ARGS(*range(1, 17), 0.5, 17, 18, 19))
+    assert ctypes.sizeof(a) == 144 and [getattr(a, n) for n, _ in a._fields_] == list(range(1, 17)) + [0.5, 17, 18, 19]
+    b = api.RmsNormBwd.from_buffer_copy(api._RMSNORM_BWD_ARGS(*range(1, 16)))
+    assert ctypes.sizeof(b) == 112 and [getattr(b, n) for n, _ in b._fields_] == list(range(1, 16))
+    c = api.Adamw.from_buffer_copy(api._ADAMW_ARGS(0.5, 0.25, 0.125, 2.0, 5, 6, 7, 8, (1 << 64) - 1, 10, 11, 12, 13))
+    assert ctypes.sizeof(c) == 88 and [getattr(c, n) for n, _ in c._fields_] == [0.5, 0.25, 0.125, 2.0, 5, 6, 7, 8, (1 << 64) - 1, 10, 11, 12, 13]
