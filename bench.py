@@ -601,6 +601,36 @@ def run_profile_case(name):
             if i >= 1: times.append(e0.elapsed_time(e1))
         print(f"{name}: {2.0 * M * N * K / (min(times) * 1e-3) / 1e12:.0f} TFLOP/s best of {len(times)}")
         return
+    if name in ("rmsnorm_fwd", "rmsnorm_bwd", "adamw_step_states32", "adamw_step_states8"):
+        # norm of 16384 x 4096 (residual added, both FP8 copies), its backward pass, an AdamW step over 24.6 M elements (bf16 gradients and copy)
+        g = torch.Generator(device=device); g.manual_seed(3)
+        rnd = lambda *s: torch.randn(*s, generator=g, device=device, dtype=torch.float32)
+        if name.startswith("rmsnorm"):
+            M, K, F8 = 16384, 4096, api.FMT_FP8_E4M3
+            x, r, gain = rnd(M, K).to(torch.bfloat16), rnd(M, K).to(torch.bfloat16), 1 + 0.1 * rnd(K)
+            out = {k: t for k, t in api.snip_rmsnorm_fwd(x, gain, 1e-5, residual=r, fmt=F8, fmt_t=F8).items() if t is not None}
+            dx, dgain = torch.empty_like(x), torch.empty(K, device=device)
+            if name == "rmsnorm_fwd":
+                call, by = lambda: api.snip_rmsnorm_fwd(x, gain, 1e-5, residual=r, fmt=F8, fmt_t=F8, out=out), 8.0625 * M * K
+            else:
+                call, by = lambda: api.snip_rmsnorm_bwd(r, x, gain, out["rstd"], dresidual=out["h"], dx=dx, dgain=dgain), 8.0 * M * K
+        else:
+            n, eight = 4096 * 6000, name.endswith("8")
+            state = torch.uint8 if eight else torch.float32
+            p, gr, c = 0.02 * rnd(n), (1e-3 * torch.exp(1.5 * rnd(n)) * rnd(n)).to(torch.bfloat16), torch.zeros(n, dtype=torch.bfloat16, device=device)
+            m, v, ms, vs = (torch.zeros(k, dtype=d, device=device) for k, d in ((n, state), (n, state), (n // 128, torch.float32), (n // 128, torch.float32)))
+            t = api.make_adamw_tensors([p], [gr], [m], [v], m_scales=[ms] if eight else None, v_scales=[vs] if eight else None, copies=[c], weight_decay=0.1)
+            call, by = lambda: api.snip_adamw_step(t, 1e-4, 0.9, 0.95, 1e-8, 10, rounding=api.ROUND_STOCHASTIC, seed=3), (16.0625 if eight else 28.0) * n
+        for i in range(4):
+            call()
+        torch.cuda.synchronize()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        for i in range(8):
+            call()
+        e1.record(); torch.cuda.synchronize()
+        print(f"{name}: {by * 8 / (e0.elapsed_time(e1) * 1e-3) / 1e9:.0f} GB/s")
+        return
     if name.startswith("adamw"):
         n = 12288 * 4096
         ms_ = [torch.randn(n, device=device) * 1e-3 for _ in range(2)]

@@ -120,38 +120,39 @@ __device__ __forceinline__ float2 sqrt2(const float2 v)
 
 __device__ __forceinline__ float2 unpack2(uint32_t b) { return make_float2(bf16lo(b), bf16hi(b)); }
 
+// What a kernel ahead may have written is read past L1 (this kernel may have started before that one ended).
 // Four consecutive elements of a lane, of which the tensor has `left` (the others read as zeros).
 __device__ __forceinline__ void load4(const void *p, uint32_t i, int left, uint2 &v)
 {
     const uint16_t *q = static_cast<const uint16_t *>(p) + i;
     if (left >= 4) {
-        v = *reinterpret_cast<const uint2 *>(q);
+        v = __ldcg(reinterpret_cast<const uint2 *>(q));
     } else {
         v = make_uint2(0u, 0u);
-        if (left > 0) v.x = q[0];
-        if (left > 1) v.x |= (uint32_t)q[1] << 16;
-        if (left > 2) v.y = q[2];
+        if (left > 0) v.x = __ldcg(q);
+        if (left > 1) v.x |= (uint32_t)__ldcg(q + 1) << 16;
+        if (left > 2) v.y = __ldcg(q + 2);
     }
 }
 __device__ __forceinline__ void load4(const void *p, uint32_t i, int left, float4 &v)
 {
     const float *q = static_cast<const float *>(p) + i;
     if (left >= 4) {
-        v = *reinterpret_cast<const float4 *>(q);
+        v = __ldcg(reinterpret_cast<const float4 *>(q));
     } else {
         v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (left > 0) v.x = q[0];
-        if (left > 1) v.y = q[1];
-        if (left > 2) v.z = q[2];
+        if (left > 0) v.x = __ldcg(q);
+        if (left > 1) v.y = __ldcg(q + 1);
+        if (left > 2) v.z = __ldcg(q + 2);
     }
 }
 __device__ __forceinline__ uint32_t load_codes(const uint8_t *p, uint32_t i, int left)
 {
-    if (left >= 4) return *reinterpret_cast<const uint32_t *>(p + i);
+    if (left >= 4) return __ldcg(reinterpret_cast<const uint32_t *>(p + i));
     uint32_t v = 0;
 #pragma unroll
     for (int j = 0; j < 3; ++j)
-        if (j < left) v |= (uint32_t)p[i + j] << (8 * j);
+        if (j < left) v |= (uint32_t)__ldcg(p + i + j) << (8 * j);
     return v;
 }
 __device__ __forceinline__ void to_floats(const uint2 &v, float2 (&f)[2]) { f[0] = unpack2(v.x); f[1] = unpack2(v.y); }
@@ -307,7 +308,7 @@ __device__ __forceinline__ void run_chunk8(const Step &s, const Chunk &c, int wa
     float *scales = second ? c.v_scale : c.m_scale;
     const uint32_t block = b0 + (lane & (U - 1));
     const bool owner = lane < 2 * U && (FULL || (int)(block * kBlock) < c.left);
-    const float scale = owner ? scales[block] : 0.0f;
+    const float scale = owner ? __ldcg(scales + block) : 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint32_t i = i0 + u * kBlock;
@@ -412,20 +413,21 @@ template <int CAP, bool P_BF16, bool G_BF16, bool BITS8, bool SR>
 __global__ void __launch_bounds__(kThreads, resident_ctas(P_BF16, BITS8, SR)) adamw_kernel(const __grid_constant__ Table<CAP> a)
 {
     __shared__ Hyper shared_hyper;
+    chain_start(CHAIN_FIRST);   // may be set up while the kernel before it on the stream ends
     const Common &c = a.c;
     Step s;
     s.h = c.h;
     uint32_t step = c.step;
     if (c.step_device || c.lr_device) {
-        int64_t t = c.step_device ? *c.step_device : c.step_host;
+        int64_t t = c.step_device ? __ldcg(reinterpret_cast<const long long *>(c.step_device)) : c.step_host;
         t = t < 1 ? 1 : t;
-        if (threadIdx.x == 0) shared_hyper = hyper(c.lr_device ? (double)*c.lr_device : c.lr, c.beta1, c.beta2, t);
+        if (threadIdx.x == 0) shared_hyper = hyper(c.lr_device ? (double)__ldcg(c.lr_device) : c.lr, c.beta1, c.beta2, t);
         __syncthreads();
         s.h = shared_hyper;
         step = (uint32_t)t;
     }
     s.b1 = c.b1; s.omb1 = c.omb1; s.b2 = c.b2; s.omb2 = c.omb2; s.eps = c.eps;
-    s.gs = c.grad_scale ? *c.grad_scale : 1.0f;
+    s.gs = c.grad_scale ? __ldcg(c.grad_scale) : 1.0f;
     s.k0 = c.k0; s.k1 = c.k1;
     s.count = 2u * step;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -457,33 +459,33 @@ int resident()
 }
 
 template <int CAP, bool P_BF16, bool G_BF16, bool BITS8, bool SR>
-void launch(const Table<CAP> &t, cudaStream_t st)
+int launch(const Table<CAP> &t, cudaStream_t st)
 {
     constexpr auto kernel = adamw_kernel<CAP, P_BF16, G_BF16, BITS8, SR>;
     const int64_t cap = (int64_t)resident<kernel>() * gemm_sm_count();
-    kernel<<<(unsigned)(t.c.chunks < cap ? t.c.chunks : cap), kThreads, 0, st>>>(t);
+    return launch_chained(kernel, (int)(t.c.chunks < cap ? t.c.chunks : cap), kThreads, 0, st, 1, t);
 }
 
 template <int CAP>
-void launch_for(const Table<CAP> &t, bool p16, bool g16, bool bits8, bool sr, cudaStream_t st)
+int launch_for(const Table<CAP> &t, bool p16, bool g16, bool bits8, bool sr, cudaStream_t st)
 {
     const int variant = (p16 ? 8 : 0) | (g16 ? 4 : 0) | (bits8 ? 2 : 0) | (sr && (p16 || bits8) ? 1 : 0);
     switch (variant) {
-        case 0: launch<CAP, false, false, false, false>(t, st); break;
-        case 2: launch<CAP, false, false, true, false>(t, st); break;
-        case 3: launch<CAP, false, false, true, true>(t, st); break;
-        case 4: launch<CAP, false, true, false, false>(t, st); break;
-        case 6: launch<CAP, false, true, true, false>(t, st); break;
-        case 7: launch<CAP, false, true, true, true>(t, st); break;
-        case 8: launch<CAP, true, false, false, false>(t, st); break;
-        case 9: launch<CAP, true, false, false, true>(t, st); break;
-        case 10: launch<CAP, true, false, true, false>(t, st); break;
-        case 11: launch<CAP, true, false, true, true>(t, st); break;
-        case 12: launch<CAP, true, true, false, false>(t, st); break;
-        case 13: launch<CAP, true, true, false, true>(t, st); break;
-        case 14: launch<CAP, true, true, true, false>(t, st); break;
-        case 15: launch<CAP, true, true, true, true>(t, st); break;
-        default: break;   // stochastic rounding of nothing: sr is dropped above
+        case 0: return launch<CAP, false, false, false, false>(t, st);
+        case 2: return launch<CAP, false, false, true, false>(t, st);
+        case 3: return launch<CAP, false, false, true, true>(t, st);
+        case 4: return launch<CAP, false, true, false, false>(t, st);
+        case 6: return launch<CAP, false, true, true, false>(t, st);
+        case 7: return launch<CAP, false, true, true, true>(t, st);
+        case 8: return launch<CAP, true, false, false, false>(t, st);
+        case 9: return launch<CAP, true, false, false, true>(t, st);
+        case 10: return launch<CAP, true, false, true, false>(t, st);
+        case 11: return launch<CAP, true, false, true, true>(t, st);
+        case 12: return launch<CAP, true, true, false, false>(t, st);
+        case 13: return launch<CAP, true, true, false, true>(t, st);
+        case 14: return launch<CAP, true, true, true, false>(t, st);
+        case 15: return launch<CAP, true, true, true, true>(t, st);
+        default: return SNIP_ERR_UNSUPPORTED;   // not reached: stochastic rounding of nothing is dropped above
     }
 }
 
@@ -502,9 +504,7 @@ int step_some(const snip_adamw_tensor_t *ts, int64_t first, int64_t count, const
     }
     if (chunks == 0) return SNIP_OK;
     t.c.chunks = (uint32_t)chunks;
-    launch_for<CAP>(t, a.param_dtype == SNIP_OUT_BF16, a.grad_dtype == SNIP_OUT_BF16, a.state_bits == 8, a.rounding == SNIP_ROUND_STOCHASTIC, st);
-    SNIP_CUDA_TRY(cudaGetLastError());
-    return SNIP_OK;
+    return launch_for<CAP>(t, a.param_dtype == SNIP_OUT_BF16, a.grad_dtype == SNIP_OUT_BF16, a.state_bits == 8, a.rounding == SNIP_ROUND_STOCHASTIC, st);
 }
 
 }  // namespace

@@ -45,7 +45,7 @@ struct NormBwdArgs {
     const void *gain;
     const float *rstd;
     uint16_t *dx;
-    float *partials;   // [groups of the grid][cols], or null
+    float *partials;   // [CTAs][cols], or null
     int32_t ld_dy, ld_h, ld_dresidual, ld_dx;
     int32_t rows, cols;
     int gain_f32, wpr;
@@ -102,11 +102,12 @@ __device__ __forceinline__ void store_codes8(uint8_t *to, const Eight &y, float 
     }
 }
 
+// (Plain loads, not the read-only path: this kernel may have started before the one that writes the gain had ended.)
 __device__ __forceinline__ Eight load_gain8(const void *gain, int f32, int col)
 {
-    if (!f32) return unpack8(__ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(gain) + col)));
-    const float4 a = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(gain) + col));
-    const float4 b = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(gain) + col) + 1);
+    if (!f32) return unpack8(*reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(gain) + col));
+    const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(gain) + col);
+    const float4 a = p[0], b = p[1];
     return {{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
 }
 
@@ -206,7 +207,6 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_kernel(const NormArgs a)
 {
     extern __shared__ __align__(128) uint8_t raw[];
     __shared__ __align__(16) float slots[2][32];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the kernel of the transposed copy, which waits for this one
     const Place at(a.wpr);
     constexpr int N = RES ? 2 : 1, kPerByte = FMT == SNIP_FMT_FP4_E2M1 ? 2 : 1;
     uint4 *const mine = reinterpret_cast<uint4 *>(raw) + threadIdx.x;
@@ -222,6 +222,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_kernel(const NormArgs a)
     }
     if (threadIdx.x < 64) slots[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
     __syncthreads();
+    chain_start(CHAIN_FIRST);
     // of the widest rows neither the gain nor the row in binary32 stays in registers
     constexpr bool kWide = V > 2 && THREADS > 512;
     auto gain_of = [&](int k) { return in[k] ? load_gain8(a.gain, a.gain_f32, at.col0 + k * at.apart) : zeros8(); };
@@ -386,7 +387,7 @@ __global__ void __launch_bounds__(kColsThreads, kColsCtas) rmsnorm_cols_kernel(c
         }
         copies_commit();
     };
-    asm volatile("griddepcontrol.wait;" ::: "memory");   // for the kernel that leaves h and rstd
+    chain_start(CHAIN_FIRST);   // h and rstd come from the kernel before this one
     int done = (int)blockIdx.x / a.tiles_c, tc = (int)blockIdx.x % a.tiles_c, buf = 0;
     fetch(0, (int)blockIdx.x, done, tc);
     for (int tile = (int)blockIdx.x; tile < a.tiles; tile += (int)gridDim.x, buf ^= 1) {
@@ -476,7 +477,6 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(const NormBwdArgs 
 {
     extern __shared__ __align__(128) uint8_t raw[];
     __shared__ __align__(16) float slots[2][32];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the reduction of the gain's gradient, which waits for this kernel
     const Place at(a.wpr);
     bool in[V];
 #pragma unroll
@@ -484,6 +484,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(const NormBwdArgs 
     const Ring<V, RES ? 3 : 2, STAGES> ring(raw, in);
     if (threadIdx.x < 64) slots[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
     __syncthreads();
+    chain_start(CHAIN_FIRST);
     const int step = (int)gridDim.x * at.groups, first = (int)blockIdx.x * at.groups, row0 = first + at.group;
     const uint16_t *py = a.dy + (int64_t)row0 * a.ld_dy + at.col0, *ph = a.h + (int64_t)row0 * a.ld_h + at.col0;
     const uint16_t *pd = RES ? a.dresidual + (int64_t)row0 * a.ld_dresidual + at.col0 : nullptr;
@@ -517,7 +518,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(const NormBwdArgs 
         dgain[k] = zeros8();
     }
     int64_t row = row0;
-    float rstd = row < a.rows ? __ldg(a.rstd + row) : 0.0f;
+    float rstd = row < a.rows ? a.rstd[row] : 0.0f;
     uint16_t *px = a.dx + (int64_t)row0 * a.ld_dx + at.col0;
     const int64_t sx = (int64_t)step * a.ld_dx;
     int parity = 0, stage = 0;
@@ -545,7 +546,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(const NormBwdArgs 
             }
         }
         row += step;
-        if (row < a.rows) rstd = __ldg(a.rstd + row);
+        if (row < a.rows) rstd = a.rstd[row];
         const float c = group_sum(dot.x + dot.y, slots[parity], at, a.wpr) * -a.inv_cols;
         if (live) {
 #pragma unroll
@@ -576,15 +577,35 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(const NormBwdArgs 
         stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
     copies_wait<0>();
-    if (a.partials) {
-        float *p = a.partials + (int64_t)row0 * a.cols + at.col0;
+    if (!a.partials) return;
+    if (at.groups > 1) {   // the groups' sums are added in order by the first one's threads, through the ring (whose copies have all arrived)
+        __syncthreads();
+        float4 *const mine = reinterpret_cast<float4 *>(raw) + threadIdx.x;
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            if (!in[k]) continue;
-            float4 *q = reinterpret_cast<float4 *>(p + k * at.apart);
-            q[0] = make_float4(dgain[k].p[0].x, dgain[k].p[0].y, dgain[k].p[1].x, dgain[k].p[1].y);
-            q[1] = make_float4(dgain[k].p[2].x, dgain[k].p[2].y, dgain[k].p[3].x, dgain[k].p[3].y);
+            mine[2 * k * blockDim.x] = make_float4(dgain[k].p[0].x, dgain[k].p[0].y, dgain[k].p[1].x, dgain[k].p[1].y);
+            mine[(2 * k + 1) * blockDim.x] = make_float4(dgain[k].p[2].x, dgain[k].p[2].y, dgain[k].p[3].x, dgain[k].p[3].y);
         }
+        __syncthreads();
+        if (at.group > 0) return;
+        for (int g = 1; g < at.groups; ++g) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float4 p = mine[2 * k * blockDim.x + 32 * a.wpr * g], q = mine[(2 * k + 1) * blockDim.x + 32 * a.wpr * g];
+                dgain[k].p[0] = __fadd2_rn(dgain[k].p[0], make_float2(p.x, p.y));
+                dgain[k].p[1] = __fadd2_rn(dgain[k].p[1], make_float2(p.z, p.w));
+                dgain[k].p[2] = __fadd2_rn(dgain[k].p[2], make_float2(q.x, q.y));
+                dgain[k].p[3] = __fadd2_rn(dgain[k].p[3], make_float2(q.z, q.w));
+            }
+        }
+    }
+    float *p = a.partials + (int64_t)blockIdx.x * a.cols + at.col0;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        if (!in[k]) continue;
+        float4 *q = reinterpret_cast<float4 *>(p + k * at.apart);
+        q[0] = make_float4(dgain[k].p[0].x, dgain[k].p[0].y, dgain[k].p[1].x, dgain[k].p[1].y);
+        q[1] = make_float4(dgain[k].p[2].x, dgain[k].p[2].y, dgain[k].p[3].x, dgain[k].p[3].y);
     }
 }
 
@@ -592,18 +613,18 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(const NormBwdArgs 
 __global__ void __launch_bounds__(1024) dgain_reduce_kernel(const float *partials, int n, int cols, float *dgain, int accumulate)
 {
     __shared__ float part[32][33];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    chain_start(CHAIN_FIRST);
     const int c = blockIdx.x * 32 + threadIdx.x;
     float v = 0.0f;
     if (c < cols)
-        for (int i = threadIdx.y; i < n; i += 32) v += partials[(int64_t)i * cols + c];
+        for (int i = threadIdx.y; i < n; i += 32) v += __ldcg(partials + (int64_t)i * cols + c);
     part[threadIdx.y][threadIdx.x] = v;
     __syncthreads();
     if (threadIdx.y == 0 && c < cols) {
         v = part[0][threadIdx.x];
 #pragma unroll
         for (int i = 1; i < 32; ++i) v += part[i][threadIdx.x];
-        dgain[c] = accumulate ? dgain[c] + v : v;
+        dgain[c] = accumulate ? __ldcg(dgain + c) + v : v;
     }
 }
 
@@ -679,15 +700,15 @@ bool bad_dims(int64_t rows, int64_t cols) { return rows < 0 || rows > INT32_MAX 
 
 constexpr int kMostSmem = 200 * 1024;
 
-// CTAs of the backward pass (each group of rows leaves one partial of dgain).  kBwdCtas bounds the workspace.
+// CTAs of the backward pass, each of which leaves one partial of dgain.  kBwdCtas bounds the workspace.
 constexpr int64_t kBwdCtas = 8 * 148;
-int64_t bwd_ctas(int64_t rows, int groups, int per_sm)
+int64_t bwd_ctas(int64_t rows, int groups, int64_t fit)
 {
-    const int64_t want = ceil_div(rows, groups), fit = (int64_t)per_sm * gemm_sm_count(), cap = fit < kBwdCtas ? fit : kBwdCtas;
+    const int64_t want = ceil_div(rows, groups), cap = fit < kBwdCtas ? fit : kBwdCtas;
     return want < cap ? want : cap;
 }
 
-// A kernel that may be set up while the one before it on the stream ends; it waits for that one's results itself.
+// Every kernel here may be set up while the one before it on the stream ends, and waits for that one before it touches memory (chain_start).
 template <typename Kernel, typename... Args>
 cudaError_t launch_behind(Kernel kernel, dim3 grid, dim3 block, int smem, cudaStream_t st, const Args &...args)
 {
@@ -756,11 +777,12 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     const Shape s = fwd_shape(t->cols, t->residual != nullptr, t->y != nullptr, a.codes != nullptr, t->rows <= kFewRows);
     a.wpr = s.wpr;
     int n = 0;   // 0: a CUDA call failed
+    cudaError_t e = cudaSuccess;
     auto launch = [&](auto v, auto threads, auto stages, auto res, auto fmt) {
         constexpr auto kernel = rmsnorm_kernel<v(), threads(), stages(), res(), fmt()>;
         n = resident<kernel>(s.threads, s.smem, kMostSmem);
         const int64_t want = ceil_div(t->rows, s.groups), cap = (int64_t)n * gemm_sm_count();
-        if (n) kernel<<<(unsigned)(want < cap ? want : cap), s.threads, s.smem, st>>>(a);
+        if (n) e = launch_behind(kernel, dim3((unsigned)(want < cap ? want : cap)), dim3(s.threads), s.smem, st, a);
     };
     auto with_fmt = [&](auto v, auto threads, auto stages, auto res) {
         if (!a.codes) launch(v, threads, stages, res, Int<SNIP_FMT_BF16>{});
@@ -774,7 +796,7 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     }
     SNIP_NORM_FWD_FORMS(SNIP_LAUNCH)
 #undef SNIP_LAUNCH
-    SNIP_CUDA_TRY(cudaGetLastError());
+    SNIP_CUDA_TRY(e);
     if (!n) return SNIP_ERR_CUDA;
     if (!t->codes_t) return SNIP_OK;
     NormColsArgs d = {};
@@ -789,7 +811,6 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     d.tiles_c = (int32_t)ceil_div(t->cols, kTile);
     d.tiles = (int32_t)(d.tiles_c * ceil_div(t->rows, kTile));
     d.gain_f32 = a.gain_f32;
-    cudaError_t e = cudaSuccess;
     auto launch_cols = [&](auto fmt) {
         constexpr auto kernel = rmsnorm_cols_kernel<fmt()>;
         constexpr int smem = (int)sizeof(ColsShared);
@@ -808,11 +829,9 @@ extern "C" int snip_rmsnorm_bwd_workspace(int64_t rows, int64_t cols, size_t *ws
     using namespace snip;
     if (!ws_bytes) return SNIP_ERR_ARG;
     if (bad_dims(rows, cols)) return SNIP_ERR_SHAPE;
-    // one partial per group of rows in flight, of the largest grid
-    const Shape s = bwd_shape(cols, 3, rows <= kFewRows);
-    int64_t groups = kBwdCtas * s.groups;
-    if (rows < groups) groups = align_up((size_t)rows, (size_t)s.groups);
-    *ws_bytes = align_up(sizeof(float) * (size_t)groups * (size_t)cols, 256);
+    // one partial per CTA of the largest grid
+    const int64_t ctas = bwd_ctas(rows, bwd_shape(cols, 3, rows <= kFewRows).groups, kBwdCtas);
+    *ws_bytes = align_up(sizeof(float) * (size_t)ctas * (size_t)cols, 256);
     return SNIP_OK;
 }
 
@@ -863,10 +882,11 @@ extern "C" int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *t, void *ws, size_t ws
     const Shape s = bwd_shape(t->cols, t->dresidual ? 3 : 2, t->rows <= kFewRows);
     a.wpr = s.wpr;
     int64_t ctas = 0;   // 0: a CUDA call failed
+    cudaError_t e = cudaSuccess;
     auto launch = [&](auto v, auto threads, auto stages, auto res) {
         constexpr auto kernel = rmsnorm_bwd_kernel<v(), threads(), stages(), res()>;
-        ctas = bwd_ctas(t->rows, s.groups, resident<kernel>(s.threads, s.smem, kMostSmem));
-        if (ctas) kernel<<<(unsigned)ctas, s.threads, s.smem, st>>>(a);
+        ctas = bwd_ctas(t->rows, s.groups, (int64_t)resident<kernel>(s.threads, s.smem, kMostSmem) * gemm_sm_count());
+        if (ctas) e = launch_behind(kernel, dim3((unsigned)ctas), dim3(s.threads), s.smem, st, a);
     };
 #define SNIP_LAUNCH(FORM, V, THREADS, STAGES)                                                   \
     if (s.form == FORM) {                                                                       \
@@ -875,11 +895,11 @@ extern "C" int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *t, void *ws, size_t ws
     }
     SNIP_NORM_BWD_FORMS(SNIP_LAUNCH)
 #undef SNIP_LAUNCH
-    SNIP_CUDA_TRY(cudaGetLastError());
+    SNIP_CUDA_TRY(e);
     if (!ctas) return SNIP_ERR_CUDA;
     if (t->dgain) {
         SNIP_CUDA_TRY(launch_behind(dgain_reduce_kernel, dim3((unsigned)ceil_div(t->cols, 32)), dim3(32, 32), 0, st, static_cast<const float *>(a.partials),
-                                    (int)(ctas * s.groups), (int)a.cols, t->dgain, (int)t->accumulate));
+                                    (int)ctas, (int)a.cols, t->dgain, (int)t->accumulate));
     }
     return SNIP_OK;
 }
