@@ -520,11 +520,12 @@ int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *args_host, void *ws, size_t ws_by
  * tensors at once.  Per element, in binary32:
  *   g' = grad * *grad_scale;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * The constants (1 - beta, bias corrections) are worked out in binary64.  All tensors of a call share param_dtype, grad_dtype and state_bits.
+ * Products and sums of the moments are rounded one by one.  The constants (1 - beta, bias corrections) are worked out in binary64.  All tensors of a call share param_dtype, grad_dtype and state_bits.
  *   param        binary32 (master weights) or bf16, updated in place
  *   param_bf16   optional: the new param rounded to nearest bf16 (what the quantizers read); binary32 params only
  *   m, v         state_bits = 32: binary32.  state_bits = 8: one E4M3 code each, blocks of 128 consecutive elements (a tensor's last
- *                may be shorter) with a binary32 scale by the rule of snip_quantize: m_scale / v_scale [ceil(n/128)];
+ *                may be shorter) with a binary32 scale each, m_scale / v_scale [ceil(n/128)]: 448 times the reciprocal of the largest
+ *                magnitude, both rounded (1 for a block of zeros, at most FLT_MAX); code = E4M3 of the binary32 product value * scale;
  *                m = value(code) / scale; v = (value(code) / scale)^2: what is coded is sqrt(v), which halves the span of magnitudes
  *                that a block has to hold, and a positive v is never given code 0 (it would turn an update into m / eps).  A scale of
  *                0 reads as a block of zeros, so that a state filled with zero bytes is a fresh one.

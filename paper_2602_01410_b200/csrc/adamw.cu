@@ -2,9 +2,10 @@
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
 // Bound by HBM: 28 bytes per element with binary32 states (p, bf16 g, m, v, bf16 copy; read and written once), 16 with 8-bit ones, which also need
-// 50 (nearest) to 70 (stochastic) instructions per element: arithmetic on pairs, a warp's loads all ahead of its arithmetic.  Fetching the next
-// chunk into shared memory meanwhile (cp.async) costs more instructions and registers than it hides (SR: 703 us in the place of 605).  Loads and
-// stores without cache hints: streaming stores cost 4 % (846 / 809 us on four 1B blocks).
+// 50 (nearest) to 75 (stochastic) instructions per element: arithmetic on pairs, a warp's loads all ahead of its arithmetic.  Fetching the next
+// chunk into shared memory meanwhile (cp.async) costs more instructions and registers than it hides (stochastic: 703 us in the place of 605, before
+// products and sums were rounded one by one, which costs 6 %).  Loads and stores without cache hints: streaming stores cost 4 % (846 / 809 us on
+// four 1B blocks).
 // The tensors' table travels in the kernel's parameters, so that a call needs no device memory of its own and a captured graph holds it;
 // a chunk of 2048 elements is the unit of work, the resident grid walks over the chunks of all tensors, and a chunk's tensor is found by
 // bisection in the table.  A warp holds 128 consecutive elements at a time, four per lane: that is a block of the 8-bit states, whose
@@ -221,21 +222,34 @@ __device__ __forceinline__ void generator(const Step &s, const Chunk &c, uint32_
     philox4x32_10((uint32_t)c.quad + (i >> 2), (uint32_t)(c.quad >> 32), s.tensor, s.count + kind, s.k0, s.k1, w);
 }
 
-// m and r = sqrt(v) (v itself in `v`), and the new weights, of four elements.
+// New moments (m, v; and r = sqrt(v)) and weights of four elements, from the old moments.  Each product and sum of the moments is rounded by
+// itself: 8-bit codes sit next to rounding borders, and what is fed back should follow from a definition that can be repeated bit for bit.
+// (The sums are scalar because a packed product and a packed sum are joined into an FMA, their .rn notwithstanding.)
 __device__ __forceinline__ void update4(const Step &s, float2 (&p)[2], const float2 (&g)[2], float2 (&m)[2], float2 (&v)[2], float2 (&r)[2])
 {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        // m, v hold b1 m and b2 v on entry
         const float2 gg = __fmul2_rn(g[j], splat(s.gs));
-        m[j] = __ffma2_rn(gg, splat(s.omb1), m[j]);
-        v[j] = __ffma2_rn(__fmul2_rn(gg, splat(s.omb2)), gg, v[j]);
+        const float2 om = __fmul2_rn(m[j], splat(s.b1)), nm = __fmul2_rn(gg, splat(s.omb1));
+        const float2 ov = __fmul2_rn(v[j], splat(s.b2)), nv = __fmul2_rn(__fmul2_rn(gg, gg), splat(s.omb2));
+        m[j] = make_float2(__fadd_rn(om.x, nm.x), __fadd_rn(om.y, nm.y));
+        v[j] = make_float2(__fadd_rn(ov.x, nv.x), __fadd_rn(ov.y, nv.y));
         r[j] = sqrt2(v[j]);
         const float2 d = __ffma2_rn(r[j], splat(s.h.inv_sqrt_bc2), splat(s.eps));
         const float2 u = __fmul2_rn(__fmul2_rn(m[j], splat(-s.h.step_size)), make_float2(rcp_fast(d.x), rcp_fast(d.y)));
         p[j] = __ffma2_rn(p[j], splat(s.keep), u);
     }
 }
+
+// Code values over their scale S, correctly rounded (Markstein's division: a product with the rounded reciprocal, corrected by its exact
+// remainder).
+__device__ __forceinline__ float2 over_scale(const float2 code, float inv, float neg_scale)
+{
+    const float2 q = __fmul2_rn(code, splat(inv));
+    return __ffma2_rn(__ffma2_rn(q, splat(neg_scale), code), splat(inv), q);
+}
+// Scale of a block: 448 times the reciprocal of its maximum, both rounded; 1 for an empty block, at most FLT_MAX.
+__device__ __forceinline__ float state_scale(float most) { return most == 0.0f ? 1.0f : fminf(448.0f * __frcp_rn(most), FLT_MAX); }
 
 template <bool FULL, bool P_BF16, bool SR>
 __device__ __forceinline__ void store_param(const Step &s, const Chunk &c, uint32_t i, int left, const float2 (&p)[2])
@@ -280,11 +294,6 @@ __device__ __forceinline__ void run_chunk32(const Step &s, const Chunk &c, int w
         to_floats(gv, g);
         to_floats(mv, m);
         to_floats(vv, v);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            m[j] = __fmul2_rn(m[j], splat(s.b1));
-            v[j] = __fmul2_rn(v[j], splat(s.b2));
-        }
         update4(s, p, g, m, v, r);
         store4<FULL>(static_cast<float *>(c.m), i, left, m);
         store4<FULL>(static_cast<float *>(c.v), i, left, v);
@@ -318,22 +327,21 @@ __device__ __forceinline__ void run_chunk8(const Step &s, const Chunk &c, int wa
         mc[u] = load_codes(static_cast<const uint8_t *>(c.m), i, left);
         vc[u] = load_codes(static_cast<const uint8_t *>(c.v), i, left);
     }
-    // b1 m = code (b1 / S);  b2 v = (code / S) (code b2 / S)
-    const float inv = scale == 0.0f ? 0.0f : __frcp_rn(scale), d1 = second ? inv : s.b1 * inv, d2 = s.b2 * inv;
+    const float inv = scale == 0.0f ? 0.0f : __frcp_rn(scale);
     float2 m[U][2], r[U][2];
     float most = 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint32_t i = i0 + u * kBlock;
-        const float b1s = __shfl_sync(kAll, d1, u), vs = __shfl_sync(kAll, d1, U + u), b2s = __shfl_sync(kAll, d2, U + u);
+        const float im = __shfl_sync(kAll, inv, u), iv = __shfl_sync(kAll, inv, U + u), nm = -__shfl_sync(kAll, scale, u), nv = -__shfl_sync(kAll, scale, U + u);
         float2 p[2], g[2], v[2];
         to_floats(pv[u], p);
         to_floats(gv[u], g);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            m[u][j] = __fmul2_rn(dec_e4m3x2(mc[u] >> (16 * j)), splat(b1s));
-            const float2 code = dec_e4m3x2(vc[u] >> (16 * j));
-            v[j] = __fmul2_rn(__fmul2_rn(code, splat(vs)), __fmul2_rn(code, splat(b2s)));
+            m[u][j] = over_scale(dec_e4m3x2(mc[u] >> (16 * j)), im, nm);
+            const float2 root = over_scale(dec_e4m3x2(vc[u] >> (16 * j)), iv, nv);
+            v[j] = __fmul2_rn(root, root);
         }
         update4(s, p, g, m[u], v, r[u]);
         store_param<FULL, P_BF16, SR>(s, c, i, FULL ? 4 : c.left - (int)i, p);
@@ -342,7 +350,7 @@ __device__ __forceinline__ void run_chunk8(const Step &s, const Chunk &c, int wa
         const uint32_t ar = __reduce_max_sync(kAll, __float_as_uint(fmaxf(fmaxf(r[u][0].x, r[u][0].y), fmaxf(r[u][1].x, r[u][1].y))));
         if ((lane & (U - 1)) == u) most = __uint_as_float(second ? ar : am);
     }
-    const float fresh = tile_scale<SNIP_FMT_FP8_E4M3>(most, 0);
+    const float fresh = state_scale(most);
     if (owner) scales[block] = fresh;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -401,9 +409,10 @@ __device__ __forceinline__ int locate(const Table<CAP> &a, uint32_t chunk, Chunk
     return lo;
 }
 
-// CTAs per SM that the registers are cut for.  A 7B block (202 M elements) in us, at five / six / seven: 8-bit states to nearest 544 / 569 / 567
-// with binary32 weights, 377 / 354 / 340 with bf16 ones; stochastic (a long run, at the power limit) 630 / 624 / 616 and 684 / 710 / 718 (two
-// generator calls per four elements: fewer registers spill).  Binary32 states: six keep 24 warps of one block each in flight; two blocks per warp or more warps are no faster.
+// CTAs per SM that the registers are cut for.  A 7B block (202 M elements) in us, at five / six / seven / eight: 8-bit states to nearest
+// 541 / 569 / - / 591 with binary32 weights, 400 / 388 / 372 / 362 with bf16 ones; stochastic (a long run, at the power limit) 667 / 660 / 657 / 660 and
+// 727 / 770 / - / 850 (two generator calls per four elements: fewer registers spill).  Binary32 states: six keep 24 warps of one block each in flight;
+// two blocks per warp or more warps are no faster.
 constexpr int resident_ctas(bool p16, bool bits8, bool sr)
 {
     return !bits8 ? 6 : p16 == sr ? 5 : 7;

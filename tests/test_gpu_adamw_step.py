@@ -282,3 +282,49 @@ def test_offsets_beyond_32_bits(api):
     for a, b in ((p[start:], q[0]), (m[start:], q[2]), (v[start:], q[3]), (ms[start // 128:], q[4]), (vs[start // 128:], q[5])):
         assert torch.equal(a, b)
     assert not torch.any(p[:start]) and torch.all(ms[:start // 128] == 1)
+
+
+@pytest.mark.parametrize("sr", [False, True])
+def test_states_are_the_definitions_bits(api, sr):
+    # 8-bit states of a chain of steps, each product and sum in binary32 as the header says: equal bit for bit, scales included (what a step
+    # rounds one way or the other is fed back, so that runs which differ in one rounding part company)
+    n, seed = 40_000, 77
+    g = torch.Generator(device="cuda").manual_seed(2)
+    size = torch.exp(2 * torch.randn(n, generator=g, device="cuda")) * 1e-3
+    p = torch.zeros(n, device="cuda")
+    m, v = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    ms, vs = torch.zeros(-(-n // 128), device="cuda"), torch.zeros(-(-n // 128), device="cuda")
+    grad = torch.zeros(n, device="cuda")
+    t = api.make_adamw_tensors([p], [grad], [m], [v], m_scales=[ms], v_scales=[vs])
+    f = np.float32
+    code_m, code_v, s_m, s_v = np.zeros(n, f), np.zeros(n, f), np.ones(len(ms), f), np.ones(len(ms), f)
+
+    def stored(x, u, floor):
+        whole = np.zeros(len(ms) * 128, f)
+        whole[:n] = np.abs(x)
+        most = whole.reshape(-1, 128).max(1)
+        s = np.where(most > 0, f(448) * (f(1) / np.where(most > 0, most, f(1))), f(1)).astype(f)
+        y = (x * np.repeat(s, 128)[:n]).astype(np.float64)
+        c = ref.nearest(y, ref.E4M3) if u is None else ref.stochastic(y, u, ref.E4M3)
+        if floor:
+            c = np.where((x > 0) & (c == 0), 2.0 ** -9, c)
+        return c.astype(f), s
+
+    for step in range(1, 7):
+        grad.copy_(torch.randn(n, generator=g, device="cuda") * size)
+        gr = grad.cpu().numpy()
+        api.snip_adamw_step(t, 1e-3, 0.9, 0.95, 1e-8, step, rounding=api.ROUND_STOCHASTIC if sr else api.ROUND_NEAREST_EVEN, seed=seed)
+        om = code_m / np.repeat(s_m, 128)[:n]
+        ov = (code_v / np.repeat(s_v, 128)[:n]) ** 2
+        nm = f(0.9) * om + f(1 - 0.9) * gr
+        nv = f(0.95) * ov + f(1 - 0.95) * (gr * gr)
+        um = uv = None
+        if sr:
+            w = ref.philox(-(-n // 4), 0, 2 * step, seed)
+            um, uv = ref.uniforms(n, w[:2]), ref.uniforms(n, w[2:])
+        assert nm.dtype == f and nv.dtype == f
+        code_m, s_m = stored(nm, um, False)
+        code_v, s_v = stored(np.sqrt(nv), uv, True)
+        assert np.array_equal(ms.cpu().numpy(), s_m) and np.array_equal(vs.cpu().numpy(), s_v)
+        assert np.array_equal(ref.code_values(m.cpu().numpy(), True, 1, n)[0].astype(f), code_m)
+        assert np.array_equal(ref.code_values(v.cpu().numpy(), True, 1, n)[0].astype(f), code_v)
