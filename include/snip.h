@@ -462,14 +462,15 @@ int snip_adamw_sensitivity(const float *m, const float *v, const void *g, int g_
  *   y       [rows][ld_y] bf16, rounded once.
  *   codes, scales      : y quantized to fmt (FP8 or FP4) on 1x128 tiles: the layout of snip_quantize, SNIP_BLOCK_ROW_1x128, as stored
  *   codes_t, scales_t  : y quantized to fmt_t on 128x1 tiles, stored transposed: SNIP_BLOCK_COL_128x1 with SNIP_Q_TRANSPOSED
- * Scale and code rule are those of snip_quantize, applied to the binary32 y and not to its bf16 rounding (one rounding less than
- * quantizing y; the codes of `codes` do not depend on which other outputs are asked for).
+ * Scale and code rule are those of snip_quantize, applied to the binary32 y and not to its bf16 rounding (one rounding less).
  * rows: any number >= 0 (0: nothing is done); cols: a multiple of 8 up to 32768; a last tile is as long as what is left.
  * With codes_t both must be multiples of 64, as the products behind it want them.  FP4 code buffers carry the slack of
  * snip_quantize_sizes.  Strides: multiples of 8, >= cols, below 2^31.
  * Inputs finite, with a sum of h^2 over a row that binary32 holds; eps > 0.  Other outputs must overlap neither each other nor an input
- * (SNIP_ERR_ARG where the same address is given twice).  No workspace.  Bytes per element: 2 (x) + 4 (residual, h) + 2 (y) + code and
- * scale bytes of each copy; with codes_t, which a second kernel makes, h is read once more.
+ * (SNIP_ERR_ARG where the same address is given twice).  A row's sum is added in an order that depends on the numbers of rows and
+ * columns and on which outputs are asked for: reruns are bit-identical, rstd of another batch size may differ in its last places.
+ * No workspace.  Bytes per element: 2 (x) + 4 (residual, h) + 2 (y) + code and scale bytes of each copy; with codes_t, which a second
+ * kernel makes, h is read once more.
  */
 typedef struct {
     const void *x;        /* bf16 [rows][ld_x] */
@@ -520,7 +521,8 @@ int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *args_host, void *ws, size_t ws_by
  * tensors at once.  Per element, in binary32:
  *   g' = grad * *grad_scale;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * Products and sums of the moments are rounded one by one.  The constants (1 - beta, bias corrections) are worked out in binary64.  All tensors of a call share param_dtype, grad_dtype and state_bits.
+ * Products and sums of the moments are rounded one by one.  The constants (1 - beta, bias corrections) are worked out in binary64.
+ * All tensors of a call share param_dtype, grad_dtype and state_bits.
  *   param        binary32 (master weights) or bf16, updated in place
  *   param_bf16   optional: the new param rounded to nearest bf16 (what the quantizers read); binary32 params only
  *   m, v         state_bits = 32: binary32.  state_bits = 8: one E4M3 code each, blocks of 128 consecutive elements (a tensor's last

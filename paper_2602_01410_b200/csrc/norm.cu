@@ -96,10 +96,10 @@ __device__ __forceinline__ void store_codes8(uint8_t *to, const Eight &y, float 
     for (int i = 0; i < 4; ++i) t[i] = __fmul2_rn(y.p[i], splat(s));
     if constexpr (FMT == SNIP_FMT_FP8_E4M3) {
         *reinterpret_cast<uint2 *>(to) = make_uint2(__byte_perm(cvt_e4m3x2(t[0].x, t[0].y), cvt_e4m3x2(t[1].x, t[1].y), 0x5410),
-                                                            __byte_perm(cvt_e4m3x2(t[2].x, t[2].y), cvt_e4m3x2(t[3].x, t[3].y), 0x5410));
+                                                   __byte_perm(cvt_e4m3x2(t[2].x, t[2].y), cvt_e4m3x2(t[3].x, t[3].y), 0x5410));
     } else {
         *reinterpret_cast<uint32_t *>(to) = cvt_e2m1x2(t[0].x, t[0].y) | cvt_e2m1x2(t[1].x, t[1].y) << 8 | cvt_e2m1x2(t[2].x, t[2].y) << 16 |
-                                                        cvt_e2m1x2(t[3].x, t[3].y) << 24;
+                                            cvt_e2m1x2(t[3].x, t[3].y) << 24;
     }
 }
 
@@ -697,7 +697,6 @@ int resident(int threads, int smem, int most_smem)
 
 bool bad_ld(int64_t ld, int64_t cols) { return ld < cols || (ld % 8) != 0 || ld > INT32_MAX; }
 bool bad_dims(int64_t rows, int64_t cols) { return rows < 0 || rows > INT32_MAX - 128 || cols <= 0 || (cols % 8) != 0 || cols > kMaxCols; }
-
 
 constexpr int kMostSmem = 200 * 1024;
 
