@@ -204,6 +204,31 @@ def test_gradient_scale_on_the_device(api):
     r.check(2, float(np.float32(0.1)), grad_scale=0.25)
 
 
+@pytest.mark.parametrize("param", [F32, BF])
+def test_gradient_scale_with_8_bit_states(api, param):
+    # no power of two: g' is rounded, which adds 1 e to the new part of m and 2 e to that of v; with the 3 e and 4 e of the two products, the
+    # constant and the sum these stay within the bounds for 8 bits (6 e and 8 e)
+    r = Run([1000, 3, 4097], 8, param, F32, False, seed=12)
+    gs = torch.tensor([0.3], device="cuda")
+    api.snip_adamw_step(r.tensors(api), HY["lr"], HY["beta1"], HY["beta2"], HY["eps"], 3, rounding=api.ROUND_STOCHASTIC, seed=2 ** 63 + 5, grad_scale=gs)
+    r.check(3, float(np.float32(0.1)), seed=2 ** 63 + 5, grad_scale=float(np.float32(0.3)))
+
+
+@pytest.mark.parametrize("on_device", ["rate", "step"])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_only_the_rate_or_only_the_step_on_the_device(api, on_device, bits):
+    a, b = Run([5000, 77], bits, F32, BF, True, seed=13), Run([5000, 77], bits, F32, BF, True, seed=13)
+    lr = torch.tensor([1e-3], device="cuda")
+    host = float(lr.cpu()[0])
+    device = (lr, 6) if on_device == "rate" else (host, torch.tensor([6], dtype=torch.int64, device="cuda"))
+    for r, (rate, step) in ((a, device), (b, (host, 6))):
+        api.snip_adamw_step(r.tensors(api), rate, 0.9, 0.95, 1e-8, step, rounding=api.ROUND_STOCHASTIC, seed=5)
+    for x, y in zip(a.m + a.v + a.ms + a.vs, b.m + b.v + b.ms + b.vs):
+        assert torch.equal(x, y)
+    for x, y in zip(a.p, b.p):      # as for the captured step: a last place of the bias corrections
+        assert torch.all((x - y).abs() <= 4 * E * y.abs() + 1e-3 * 8 * E)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_captured_step_reads_step_and_rate_at_each_replay(api, bits):
     r, w = Run([5000, 77], bits, F32, BF, True, seed=10), Run([5000, 77], bits, F32, BF, True, seed=10)

@@ -97,6 +97,18 @@ def test_both_copies(api, rows, cols, residual, fp8, fp8_t):
     assert np.all(np.abs(f64(t["y"]) - y) <= (2.0 ** -8 + 40 * E) * np.abs(y))
 
 
+@pytest.mark.parametrize("rows,cols", [(64, 192), (320, 576), (448, 4096)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_everything_at_once(api, rows, cols, residual):
+    x, res, gain = rand(rows, cols, 8), rand(rows, cols, 9) if residual else None, gain_of(cols, True)
+    o = api.snip_rmsnorm_fwd(x, gain, EPS, residual=res, fmt=api.FMT_FP4_E2M1, fmt_t=api.FMT_FP8_E4M3, want_y=True)
+    h, rstd, y = ref.norm(f64(x), None if res is None else f64(res), f64(gain), EPS)
+    assert np.array_equal(f64(o["h"]), h) and np.all(np.abs(f64(o["rstd"]) - rstd) <= 36 * E * rstd)
+    assert np.all(np.abs(f64(o["y"]) - y) <= (2.0 ** -8 + 40 * E) * np.abs(y))
+    check_codes(o["codes"], o["scales"], y, False, False)
+    check_codes(o["codes_t"], o["scales_t"], y, True, True)
+
+
 @pytest.mark.parametrize("rows,cols,form", [(257, 512, "row"), (5000, 4096, "row"), (2049, 200, "row"), (4096, 1024, "dual"), (20480, 128, "dual")])
 def test_many_rows(api, rows, cols, form):
     # more rows than the grid holds at a time: groups walk on; a few rows and columns of the result are compared
