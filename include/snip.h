@@ -539,7 +539,9 @@ int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *args_host, void *ws, size_t ws_by
  * step >= 1 counts this step.  step_device, lr_device (device, may be NULL) take the place of step and lr: a captured graph then reads
  * the current values at each replay (a *step_device below 1 counts as 1).  grad_scale (device, may be NULL = 1): inverse loss scale, clipping factor.
  * eps: a normal binary32 number.  The root of a v below 2^-126 comes out too small (0 stays 0).
- * Alignment: 16 bytes, scales 4.  n: any, 0 included.  Inputs finite.  The tensors must not overlap each other (what is written is
+ * A g' whose square passes FLT_MAX (|g'| > 1.8e19) makes v infinite: the update is then m / inf = 0 and param only decays.  A binary32 v stays
+ * infinite; an 8-bit state holds sqrt(FLT_MAX) in the place of the infinite root and comes down again.
+ * Alignment: 16 bytes, scales 4.  n: any, 0 included.  Inputs finite, grad * *grad_scale too.  The tensors must not overlap each other (what is written is
  * written once).  No workspace; one launch per 448 tensors, read and written once per element.
  */
 typedef struct {

@@ -107,10 +107,19 @@ __device__ __forceinline__ float rcp_fast(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// Square roots to half a last place: v times its approximate reciprocal root, and a Newton step.  (Below 2^-126, where the reciprocal root is
-// held at 2^63, too small; 0 for 0.)
-__device__ __forceinline__ float2 sqrt2(const float2 v)
+// At most FLT_MAX; NaN stays NaN.
+__device__ __forceinline__ float at_most_flt_max(float x)
 {
+    float r;
+    asm("min.NaN.f32 %0, %1, 0f7F7FFFFF;" : "=f"(r) : "f"(x));
+    return r;
+}
+// Square roots to half a last place: v times its approximate reciprocal root, and a Newton step.  (Below 2^-126, where the reciprocal root is
+// held at 2^63, too small; 0 for 0.  Of an infinite v, which the square of a finite gradient can make: that of FLT_MAX, so that an 8-bit
+// state stays finite.)
+__device__ __forceinline__ float2 sqrt2(float2 v)
+{
+    v = make_float2(at_most_flt_max(v.x), at_most_flt_max(v.y));
     float2 y;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, FLT_MIN)));
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(v.y, FLT_MIN)));
@@ -235,7 +244,9 @@ __device__ __forceinline__ void update4(const Step &s, float2 (&p)[2], const flo
         m[j] = make_float2(__fadd_rn(om.x, nm.x), __fadd_rn(om.y, nm.y));
         v[j] = make_float2(__fadd_rn(ov.x, nv.x), __fadd_rn(ov.y, nv.y));
         r[j] = sqrt2(v[j]);
-        const float2 d = __ffma2_rn(r[j], splat(s.h.inv_sqrt_bc2), splat(s.eps));
+        // the root that the weight sees is infinite where v is: for any other v the addend is less than 2^-62 of the root and leaves it as it is
+        const float2 root = __ffma2_rn(v[j], splat(FLT_MIN), r[j]);
+        const float2 d = __ffma2_rn(root, splat(s.h.inv_sqrt_bc2), splat(s.eps));
         const float2 u = __fmul2_rn(__fmul2_rn(m[j], splat(-s.h.step_size)), make_float2(rcp_fast(d.x), rcp_fast(d.y)));
         p[j] = __ffma2_rn(p[j], splat(s.keep), u);
     }
