@@ -74,7 +74,8 @@ __host__ __device__ inline Hyper hyper(double lr, double beta1, double beta2, in
 // the neighbouring grid points and u the 16-bit uniform, hi iff (a - lo)/(hi - lo) > (u + 1/2)/2^16.  On the bits, as for E2M1: from 2^-6 up a
 // grid point has 20 zero bits at its end, and their value f exceeds 16 u + 8 iff f + 16 (65535 - u) + 7 carries out of them; below, the same
 // holds for a + 2^-6, rounded upwards.  t comes from a block scaled by its own maximum: it passes 448 by a few last places at most, which
-// leave the largest addend 9 units short of a carry.  SIGNED = false: t >= 0.
+// leave the largest addend 9 units short of a carry.  SIGNED = false: t >= 0.  NaN is 0x7FFFFFFF, which the addition carries round to a zero;
+// 0 s + v makes it NaN again.
 template <bool SIGNED>
 __device__ __forceinline__ float2 sr_e4m3x2(const float2 t, uint32_t w)
 {
@@ -85,14 +86,16 @@ __device__ __forceinline__ float2 sr_e4m3x2(const float2 t, uint32_t w)
     const float2 s = __ffma2_ru(off, make_float2(0.015625f, 0.015625f), a);
     const uint32_t r0 = ((~w << 4) & 0xFFFF0u) | 7u, r1 = ((~w >> 12) & 0xFFFF0u) | 7u;
     const float2 q = make_float2(__uint_as_float((__float_as_uint(s.x) + r0) & 0xFFF00000u), __uint_as_float((__float_as_uint(s.y) + r1) & 0xFFF00000u));
-    const float2 v = __ffma2_rn(off, make_float2(-0.015625f, -0.015625f), q);
+    const float2 v = __ffma2_rn(s, make_float2(0.0f, 0.0f), __ffma2_rn(off, make_float2(-0.015625f, -0.015625f), q));
     return SIGNED ? make_float2(copysignf(v.x, t.x), copysignf(v.y, t.y)) : v;
 }
-// ... to bf16 bits, packed: the low 16 bits f exceed u + 1/2 iff f + 65535 - u carries.
+// ... to bf16 bits, packed: the low 16 bits f exceed u + 1/2 iff f + 65535 - u carries, which is what the conversion's random bits do (equal to the
+// integer addition on 2^31 pairs, subnormal and the largest ones among them).  It keeps a NaN, which the addition would carry round to -0.
 __device__ __forceinline__ uint32_t sr_bf16x2(const float2 t, uint32_t w)
 {
-    const uint32_t lo = __float_as_uint(t.x) + (~w & 0xFFFFu), hi = __float_as_uint(t.y) + (~w >> 16);
-    return __byte_perm(lo, hi, 0x7632);
+    uint32_t r;
+    asm("cvt.rs.bf16x2.f32 %0, %1, %2, %3;" : "=r"(r) : "f"(t.y), "f"(t.x), "r"(~w));
+    return r;
 }
 __device__ __forceinline__ uint32_t rn_bf16x2(const float2 t)
 {

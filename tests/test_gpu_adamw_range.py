@@ -135,3 +135,59 @@ def test_a_square_within_the_range_is_an_ordinary_one(api, bits):
     a.step(1, False)
     p, *_ = ref.adamw(np.array([before]), np.array([float(a.g[9])]), np.zeros(1), np.zeros(1), LR, B1, B2, EPS, 1, float(np.float32(WD)))
     assert abs(float(a.p[9]) - p[0]) <= 4 * E * before + 20 * E * LR
+
+
+@pytest.mark.parametrize("bits,param,grad,sr", FORMS)
+@pytest.mark.parametrize("n", [N, LONG])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_no_rounding_hides_what_is_not_a_number(api, bits, param, grad, sr, n, what):
+    # outside the documented range, but a step that has diverged must not look like a sound one
+    at = [5, 140, n - 1]
+    a, b = State(api, n, bits, param, grad), State(api, n, bits, param, grad)
+    a.g[at], b.g[at] = what, 0.0
+    others = np.setdiff1d(np.arange(n), at)
+    for k in (1, 2):                    # and it stays one
+        a.step(k, sr)
+        b.step(k, sr)
+        a.g[at] = 1e-3
+        assert np.all(np.isnan(a.p.double().cpu().numpy()[at]))
+        if a.c is not None:
+            assert np.all(np.isnan(a.c.double().cpu().numpy()[at]))
+        if bits == 32 or np.isnan(what):
+            assert not np.any(np.isfinite(a.values("m")[at]))
+        if bits == 32:
+            assert not np.any(np.isfinite(a.values("v")[at]))
+        elif np.isnan(what):
+            assert np.all(np.isnan(a.values("v")[at]))
+        assert torch.equal(a.p[others], b.p[others]) or np.isinf(what)
+        if k == 1:
+            assert torch.equal(a.p[others], b.p[others])
+        if np.isnan(what):
+            # the scale is that of the block's numbers: the other elements are what they are without it
+            for name in ("m", "v"):
+                assert torch.equal(getattr(a, name)[others], getattr(b, name)[others])
+            assert torch.equal(a.ms, b.ms) and torch.equal(a.vs, b.vs)
+
+
+@pytest.mark.parametrize("bits,param,grad,sr", FORMS)
+def test_a_weight_that_is_not_a_number_stays_one(api, bits, param, grad, sr):
+    a, b = State(api, N, bits, param, grad), State(api, N, bits, param, grad)
+    a.p[[5, 299]] = float("nan")
+    a.p[6] = float("inf")
+    a.step(1, sr)
+    b.step(1, sr)
+    got = a.p.double().cpu().numpy()
+    assert np.all(np.isnan(got[[5, 299]])) and np.isposinf(got[6])
+    others = [i for i in range(N) if i not in (5, 6, 299)]
+    assert torch.equal(a.p[others], b.p[others]) and torch.equal(a.m, b.m) and torch.equal(a.v, b.v)
+
+
+@pytest.mark.parametrize("sr", [False, True])
+def test_the_largest_weights_round_as_their_type_does(api, sr):
+    # no update and no decay: bf16 weights come back as they are, the largest finite ones and both zeros included
+    p = torch.tensor([3.3895e38, -3.3895e38, 0.0, -0.0, 1.0, 2.0 ** -126, -2.0 ** -133], device="cuda").to(BF)
+    keep = p.clone()
+    g, m, v = (torch.zeros(7, device="cuda") for _ in range(3))
+    t = api.make_adamw_tensors([p], [g], [m], [v])
+    api.snip_adamw_step(t, 0.0, B1, B2, EPS, 1, rounding=api.ROUND_STOCHASTIC if sr else api.ROUND_NEAREST_EVEN, seed=5)
+    assert torch.equal(p, keep)
