@@ -423,14 +423,16 @@ __device__ __forceinline__ int locate(const Table<CAP> &a, uint32_t chunk, Chunk
     return lo;
 }
 
-// CTAs per SM that the registers are cut for.  A 7B block (202 M elements) in us, at five / six / seven / eight: 8-bit states to nearest
-// 541 / 569 / - / 591 with binary32 weights, 400 / 388 / 372 / 362 with bf16 ones; stochastic (a long run, at the power limit) 667 / 660 / 657 / 660 and
-// 727 / 770 / - / 850 (two generator calls per four elements: fewer registers spill).  Binary32 states: six keep 24 warps of one block each in flight;
-// two blocks per warp or more warps are no faster.
+// CTAs per SM that the registers of the forms with 8-bit states are cut for.  A 7B block (202 M elements) in us, at four / five / six / seven / eight,
+// bf16 gradients: to nearest 559 / 543 / 567 / 579 / 598 with binary32 weights, 443 / 424 / 398 / 393 / 382 with bf16 ones; stochastic 679 / 656 / 646 /
+// 645 / 645 and 734 / 745 / 767 / 799 / 816 (two generator calls per four elements: the more registers, the fewer spill).
 constexpr int resident_ctas(bool p16, bool bits8, bool sr)
 {
-    return !bits8 ? 6 : p16 == sr ? 5 : 7;
+    return !bits8 ? 6 : p16 ? (sr ? 4 : 8) : (sr ? 7 : 5);
 }
+// Most CTAs per SM that are launched, 0 for all that fit.  With binary32 states the registers leave room for eight to ten; four blocks of the 1B model
+// in us, at six / at all: binary32 weights 793 / 820, bf16 ones 637 / 624, and stochastic 656 / 610.
+constexpr int launched_ctas(bool p16, bool bits8) { return !bits8 && !p16 ? 6 : 0; }
 
 template <int CAP, bool P_BF16, bool G_BF16, bool BITS8, bool SR>
 __global__ void __launch_bounds__(kThreads, resident_ctas(P_BF16, BITS8, SR)) adamw_kernel(const __grid_constant__ Table<CAP> a)
@@ -485,7 +487,9 @@ template <int CAP, bool P_BF16, bool G_BF16, bool BITS8, bool SR>
 int launch(const Table<CAP> &t, cudaStream_t st)
 {
     constexpr auto kernel = adamw_kernel<CAP, P_BF16, G_BF16, BITS8, SR>;
-    const int64_t cap = (int64_t)resident<kernel>() * gemm_sm_count();
+    constexpr int most = launched_ctas(P_BF16, BITS8);
+    const int fit = resident<kernel>();
+    const int64_t cap = (int64_t)(most && most < fit ? most : fit) * gemm_sm_count();
     return launch_chained(kernel, (int)(t.c.chunks < cap ? t.c.chunks : cap), kThreads, 0, st, 1, t);
 }
 
