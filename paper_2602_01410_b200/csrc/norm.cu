@@ -638,12 +638,12 @@ struct Shape {
 // More vectors per thread spread what a row costs over more elements; fewer leave more threads to fetch.  16384 x 4096 with two / four vectors in us:
 // residual added 65.3 / 63.4, and y written 91.8 / 89.4, and FP8 codes 83.0 / 83.1 (8192 x 8192: 79.7 / 83.1); no residual: rstd alone 21.5 / 23.8,
 // y 47.5 / 43.7, codes 41.6 / 37.9.  2048 columns: 21.3 / 22.2.
-Shape fwd_shape(int64_t cols, bool residual, bool y, bool codes, bool few)
+constexpr Shape fwd_shape(int64_t cols, bool residual, bool y, bool codes, bool few)
 {
-    Shape s;
+    Shape s = {};
     const bool four = cols > 2048 && (residual ? !codes : codes || y);
     s.v = cols > 8192 ? 4 : few ? 1 : four ? 4 : 2;
-    s.wpr = (int)ceil_div(cols, 256 * s.v);
+    s.wpr = (int)((cols + 256 * s.v - 1) / (256 * s.v));
     s.threads = s.wpr <= 8 ? 256 : s.wpr <= 16 ? 512 : 1024;
     s.groups = s.threads / 32 / s.wpr;
     s.form = s.v == 1 ? (s.threads == 256 ? 0 : s.threads == 512 ? 1 : 2) : s.v == 2 ? (s.threads == 256 ? 3 : 4) : s.threads == 512 ? 5 : s.threads == 1024 ? 6 : 7;
@@ -653,11 +653,11 @@ Shape fwd_shape(int64_t cols, bool residual, bool y, bool codes, bool few)
 }
 // Backward: as F(form, V, most threads, stages).
 #define SNIP_NORM_BWD_FORMS(F) F(0, 1, 1024, 3) F(1, 2, 512, 3) F(2, 2, 512, 2) F(3, 4, 512, 2) F(4, 4, 1024, 1)
-Shape bwd_shape(int64_t cols, int arrays, bool few)
+constexpr Shape bwd_shape(int64_t cols, int arrays, bool few)
 {
-    Shape s;
+    Shape s = {};
     s.v = cols > 8192 ? 4 : few ? 1 : 2;
-    s.wpr = (int)ceil_div(cols, 256 * s.v);
+    s.wpr = (int)((cols + 256 * s.v - 1) / (256 * s.v));
     s.groups = s.wpr >= 8 ? 1 : 8 / s.wpr;
     s.threads = 32 * s.wpr * s.groups;
     const int row_bytes = arrays * s.v * s.threads * 16;
@@ -667,6 +667,22 @@ Shape bwd_shape(int64_t cols, int arrays, bool few)
     return s;
 }
 constexpr int64_t kFewRows = 296;
+// Whether a call reaches a form with a residual (gradient) and, forward, with row codes: only such kernels are built.  Every width of a vector group
+// is looked at, the rules change nowhere else.
+constexpr bool fwd_reaches(int form, bool residual, bool codes)
+{
+    for (int64_t cols = 256; cols <= kMaxCols; cols += 256)
+        for (int i = 0; i < 4; ++i)
+            if (fwd_shape(cols, residual, (i & 1) != 0, codes, (i & 2) != 0).form == form) return true;
+    return false;
+}
+constexpr bool bwd_reaches(int form, bool residual)
+{
+    for (int64_t cols = 256; cols <= kMaxCols; cols += 256)
+        for (int few = 0; few < 2; ++few)
+            if (bwd_shape(cols, residual ? 3 : 2, few != 0).form == form) return true;
+    return false;
+}
 
 // CTAs of a kernel that an SM holds, with its dynamic shared memory allowed for (asked once: the same on every device of this family; the
 // allowance is per device).
@@ -778,21 +794,23 @@ extern "C" int snip_rmsnorm_fwd(const snip_rmsnorm_t *t, void *stream)
     a.wpr = s.wpr;
     int n = 0;   // 0: a CUDA call failed
     cudaError_t e = cudaSuccess;
-    auto launch = [&](auto v, auto threads, auto stages, auto res, auto fmt) {
-        constexpr auto kernel = rmsnorm_kernel<v(), threads(), stages(), res(), fmt()>;
-        n = resident<kernel>(s.threads, s.smem, kMostSmem);
-        const int64_t want = ceil_div(t->rows, s.groups), cap = (int64_t)n * gemm_sm_count();
-        if (n) e = launch_behind(kernel, dim3((unsigned)(want < cap ? want : cap)), dim3(s.threads), s.smem, st, a);
+    auto launch = [&](auto form, auto v, auto threads, auto stages, auto res, auto fmt) {
+        if constexpr (fwd_reaches(form(), res(), fmt() != SNIP_FMT_BF16)) {
+            constexpr auto kernel = rmsnorm_kernel<v(), threads(), stages(), res(), fmt()>;
+            n = resident<kernel>(s.threads, s.smem, kMostSmem);
+            const int64_t want = ceil_div(t->rows, s.groups), cap = (int64_t)n * gemm_sm_count();
+            if (n) e = launch_behind(kernel, dim3((unsigned)(want < cap ? want : cap)), dim3(s.threads), s.smem, st, a);
+        }
     };
-    auto with_fmt = [&](auto v, auto threads, auto stages, auto res) {
-        if (!a.codes) launch(v, threads, stages, res, Int<SNIP_FMT_BF16>{});
-        else if (t->fmt == SNIP_FMT_FP8_E4M3) launch(v, threads, stages, res, Int<SNIP_FMT_FP8_E4M3>{});
-        else launch(v, threads, stages, res, Int<SNIP_FMT_FP4_E2M1>{});
+    auto with_fmt = [&](auto form, auto v, auto threads, auto stages, auto res) {
+        if (!a.codes) launch(form, v, threads, stages, res, Int<SNIP_FMT_BF16>{});
+        else if (t->fmt == SNIP_FMT_FP8_E4M3) launch(form, v, threads, stages, res, Int<SNIP_FMT_FP8_E4M3>{});
+        else launch(form, v, threads, stages, res, Int<SNIP_FMT_FP4_E2M1>{});
     };
-#define SNIP_LAUNCH(FORM, V, THREADS, STAGES)                                                   \
-    if (s.form == FORM) {                                                                       \
-        if (t->residual) with_fmt(Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::true_type{});   \
-        else with_fmt(Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::false_type{});              \
+#define SNIP_LAUNCH(FORM, V, THREADS, STAGES)                                                              \
+    if (s.form == FORM) {                                                                                  \
+        if (t->residual) with_fmt(Int<FORM>{}, Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::true_type{}); \
+        else with_fmt(Int<FORM>{}, Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::false_type{});            \
     }
     SNIP_NORM_FWD_FORMS(SNIP_LAUNCH)
 #undef SNIP_LAUNCH
@@ -883,15 +901,17 @@ extern "C" int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *t, void *ws, size_t ws
     a.wpr = s.wpr;
     int64_t ctas = 0;   // 0: a CUDA call failed
     cudaError_t e = cudaSuccess;
-    auto launch = [&](auto v, auto threads, auto stages, auto res) {
-        constexpr auto kernel = rmsnorm_bwd_kernel<v(), threads(), stages(), res()>;
-        ctas = bwd_ctas(t->rows, s.groups, (int64_t)resident<kernel>(s.threads, s.smem, kMostSmem) * gemm_sm_count());
-        if (ctas) e = launch_behind(kernel, dim3((unsigned)ctas), dim3(s.threads), s.smem, st, a);
+    auto launch = [&](auto form, auto v, auto threads, auto stages, auto res) {
+        if constexpr (bwd_reaches(form(), res())) {
+            constexpr auto kernel = rmsnorm_bwd_kernel<v(), threads(), stages(), res()>;
+            ctas = bwd_ctas(t->rows, s.groups, (int64_t)resident<kernel>(s.threads, s.smem, kMostSmem) * gemm_sm_count());
+            if (ctas) e = launch_behind(kernel, dim3((unsigned)ctas), dim3(s.threads), s.smem, st, a);
+        }
     };
-#define SNIP_LAUNCH(FORM, V, THREADS, STAGES)                                                   \
-    if (s.form == FORM) {                                                                       \
-        if (t->dresidual) launch(Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::true_type{});    \
-        else launch(Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::false_type{});                \
+#define SNIP_LAUNCH(FORM, V, THREADS, STAGES)                                                              \
+    if (s.form == FORM) {                                                                                  \
+        if (t->dresidual) launch(Int<FORM>{}, Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::true_type{});  \
+        else launch(Int<FORM>{}, Int<V>{}, Int<THREADS>{}, Int<STAGES>{}, std::false_type{});              \
     }
     SNIP_NORM_BWD_FORMS(SNIP_LAUNCH)
 #undef SNIP_LAUNCH
