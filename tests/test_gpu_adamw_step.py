@@ -353,3 +353,16 @@ def test_states_are_the_definitions_bits(api, sr):
         assert np.array_equal(ms.cpu().numpy(), s_m) and np.array_equal(vs.cpu().numpy(), s_v)
         assert np.array_equal(ref.code_values(m.cpu().numpy(), True, 1, n)[0].astype(f), code_m)
         assert np.array_equal(ref.code_values(v.cpu().numpy(), True, 1, n)[0].astype(f), code_v)
+
+
+def test_a_list_in_one_call_and_in_several(api):
+    # the optimizer step to nearest: a tensor's result does not depend on its place in the list, nor on how lists are cut
+    for bits in (32, 8):
+        a, b = Run(SIZES, bits, F32, BF, True, seed=14), Run(SIZES, bits, F32, BF, True, seed=14)
+        api.snip_adamw_step(a.tensors(api), HY["lr"], HY["beta1"], HY["beta2"], HY["eps"], 3)
+        for at in (slice(5, None), slice(0, 2), slice(2, 5)):
+            eight = bits == 8
+            t = api.make_adamw_tensors(b.p[at], b.g[at], b.m[at], b.v[at], m_scales=b.ms[at] if eight else None, v_scales=b.vs[at] if eight else None, copies=b.c[at], weight_decay=0.1)
+            api.snip_adamw_step(t, HY["lr"], HY["beta1"], HY["beta2"], HY["eps"], 3)
+        for x, y in zip(a.p + a.m + a.v + a.ms + a.vs + a.c, b.p + b.m + b.v + b.ms + b.vs + b.c):
+            assert np.array_equal(x.float().cpu().numpy(), y.float().cpu().numpy())
