@@ -1,11 +1,12 @@
 // One AdamW step over many tensors at once, states in 32 or 8 bits.
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
-// Bound by HBM: 28 bytes per element with binary32 states (p, bf16 g, m, v, bf16 copy; read and written once), 16 with 8-bit ones, which also need
-// 50 (nearest) to 75 (stochastic) instructions per element: arithmetic on pairs, a warp's loads all ahead of its arithmetic.  Fetching the next
-// chunk into shared memory meanwhile (cp.async) costs more instructions and registers than it hides (stochastic: 703 us in the place of 605, before
-// products and sums were rounded one by one, which costs 6 %).  Loads and stores without cache hints: streaming stores cost 4 % (846 / 809 us on
-// four 1B blocks).
+// Binary32 states: 28 bytes per element (p, bf16 g, m, v, bf16 copy; read and written once), bound by HBM; four 1B blocks 795-834 us, 90-95 % of
+// the copy rate.  8-bit states: 16 bytes; to nearest still HBM (a 7B block 541 us, 92 %), stochastic 71 instructions per element, bound by issue slots
+// (62 % busy) and the power cap (644 us, 715 in a long run).  Hence arithmetic on pairs and a warp's loads all ahead of its arithmetic.  Fetching
+// the next chunk into shared memory meanwhile (cp.async) costs more instructions and registers than it hides (stochastic 605 -> 703 us when it was
+// measured; since then products and sums rounded one by one cost 6 %, the root of an infinite v and NaN through the rounding 3 %).  Loads and stores
+// without cache hints: streaming stores cost 4 % (846 / 809 us on four 1B blocks).
 // The tensors' table travels in the kernel's parameters, so that a call needs no device memory of its own and a captured graph holds it;
 // a chunk of 2048 elements is the unit of work, the resident grid walks over the chunks of all tensors, and a chunk's tensor is found by
 // bisection in the table.  A warp holds 128 consecutive elements at a time, four per lane: that is a block of the 8-bit states, whose
@@ -431,7 +432,8 @@ constexpr int resident_ctas(bool p16, bool bits8, bool sr)
     return !bits8 ? 6 : p16 ? (sr ? 4 : 8) : (sr ? 7 : 5);
 }
 // Most CTAs per SM that are launched, 0 for all that fit.  With binary32 states the registers leave room for eight to ten; four blocks of the 1B model
-// in us, at six / at all: binary32 weights 793 / 820, bf16 ones 637 / 624, and stochastic 656 / 610.
+// in us, at six / at all: binary32 weights 793 / 820 (one call at a time 796 / 855; calls that follow each other on three states 833 / 832), bf16
+// ones 637 / 624, and stochastic 656 / 610.
 constexpr int launched_ctas(bool p16, bool bits8) { return !bits8 && !p16 ? 6 : 0; }
 
 template <int CAP, bool P_BF16, bool G_BF16, bool BITS8, bool SR>

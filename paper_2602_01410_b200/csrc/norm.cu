@@ -3,12 +3,17 @@
 //             on 128x1 tiles stored transposed, by the quantizers' scale rule
 //   backward: g = dy gain, c = mean(g h rstd), dx = rstd (g - h rstd c) + dresidual, dgain = sum over rows of dy h rstd
 //
-// All of it is bound by HBM: a few operations per element against 6 to 10 bytes.  16384 x 4096, bf16 gain, in us (TB/s, of 6.55 for a copy): residual
-// added and FP8 row codes 80-83 (5.7), the transposed codes too 110 (4.9; 6.1 with h's second reading), backward with a residual gradient 82 (6.5).
+// Bound by HBM where a residual is read: a few operations per element against 6 to 10 bytes; without one (3 bytes with codes) issue slots come
+// next to it: 83 % of the copy rate.  16384 x 4096, bf16 gain, in us (TB/s, of 6.55 for a copy): residual
+// added and FP8 row codes 80-83 (5.7), the transposed codes too 110 (4.9; 6.1 with h's second reading), both in FP4 97 (4.9; 6.2), backward with a residual
+// gradient 82 (6.5), without 66 (6.1).
 //
 // rmsnorm_kernel / rmsnorm_bwd_kernel: a group of warps owns a row at a time and a thread the same columns of each of its rows, so that
-// the gain (and the gain's gradient) stays in registers; the grid is resident and walks over the rows.  The row is read once: it stays in
-// registers between the reduction and the outputs, and the next rows are on their way during both.
+// the gain's gradient (and, but for the widest rows, the gain) stays in registers; the grid is resident and walks over the rows.  The row is read
+// once: it stays in registers between the reduction and the outputs, and the next rows are on their way during both: a ring of three stages fetches
+// two rows ahead, one of two one, one of a single stage (forward and backward beyond 16384 columns) none.  The forms with four vectors per thread of
+// the backward pass and the 1024-thread one of the forward pass, beyond 8192 and 16384 columns, load the gain again for each row; that backward
+// pass also takes the row from shared memory a second time, and that forward pass keeps it in bf16.
 #include <cuda_bf16.h>
 #include <float.h>
 
@@ -721,7 +726,8 @@ bool bad_dims(int64_t rows, int64_t cols) { return rows < 0 || rows > INT32_MAX 
 
 constexpr int kMostSmem = 200 * 1024;
 
-// CTAs of the backward pass, each of which leaves one partial of dgain.  kBwdCtas bounds the workspace.
+// CTAs of the backward pass, each of which leaves one partial of dgain.  kBwdCtas bounds the workspace, which is asked for without a device: eight per
+// SM of this chip, of which fewer fit (16384 x 4096: 19.4 MB, of which 296 CTAs use 4.8).
 constexpr int64_t kBwdCtas = 8 * 148;
 int64_t bwd_ctas(int64_t rows, int groups, int64_t fit)
 {
