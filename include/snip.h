@@ -541,7 +541,7 @@ int snip_rmsnorm_bwd(const snip_rmsnorm_bwd_t *args_host, void *ws, size_t ws_by
  * eps: a normal binary32 number.  The root of a v below 2^-126 comes out too small (0 stays 0).
  * A g' whose square passes FLT_MAX (|g'| > 1.8e19) makes v infinite: the update is then m / inf = 0 and param only decays.  A binary32 v stays
  * infinite; an 8-bit state holds sqrt(FLT_MAX) in the place of the infinite root and comes down again.  No rounding hides a NaN that comes in:
- * param, its copy and the codes are NaN then.
+ * what it enters (param, its copy, codes) is NaN.
  * Alignment: 16 bytes, scales 4.  n: any, 0 included.  Inputs finite, grad * *grad_scale too.  The tensors must not overlap each other (what is written is
  * written once).  No workspace; one launch per 448 tensors, read and written once per element.
  */
